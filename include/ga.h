@@ -261,6 +261,130 @@ int ga_backward(ga_shape_t s, const void *Q, const void *dO, const int32_t *belo
                 void *workspace, size_t workspace_bytes, void *stream);
 
 /*
+ * Linear attention with a decay for each head: an order-aware, causal
+ * attention whose cost per token does not grow with the sequence, in place of
+ * the group attention above.  Per (batch, query head) slice, with
+ * l = exp(log_decay[h]) and a 64 x 64 state S (key feature by value feature):
+ *   S_t = l S_{t-1} + k_t v_t^T,   o_t = scale S_t^T q_t.
+ *   s          shape of Q and O: [B,H,n,64].
+ *   Hk         heads of K and V, [B,Hk,n,64]: Hk divides H, and query head h
+ *              reads key head h / (H / Hk).
+ *   log_decay  [H] fp32, each in [-inf, 0] (not checked): constants of the
+ *              layer, no gradient is formed for them.
+ *   lengths    optional [B] int32: batch b has lengths[b] tokens (values
+ *              outside [0, n] are clamped).  Rows of the inputs behind them are
+ *              not read; those of the outputs and gradients are set to zero.
+ *   state      optional [B,H,64,64] fp32: S before the first token (NULL: 0).
+ *   out_state  optional: S behind the last token (may be `state` itself).
+ * Products are accumulated, and the state is kept, in fp32; bf16 outputs are
+ * rounded once.  Accuracy versus the fp64 definition: 1e-5 (GA_F32 and every
+ * state), 5e-3 (GA_BF16), each as the 2-norm of the error over the result's.
+ * Every reduction has a fixed order: repeated calls give identical bits.
+ * Pointer, stream and error conventions as above (4-byte alignment is enough
+ * for log_decay and lengths); the workspace is ga_linear_workspace_bytes
+ * (0: none needed, the pointer may then be NULL).  Outputs must not overlap
+ * inputs, except as stated.
+ */
+size_t ga_linear_workspace_bytes(ga_shape_t s, int32_t Hk);
+int ga_linear_attend(ga_shape_t s, int32_t Hk, const void *Q, const void *K, const void *V, const float *log_decay,
+                     const int32_t *lengths, const float *state, float scale, void *O, float *out_state,
+                     void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Gradient of ga_linear_attend with respect to Q, K, V and the initial state.
+ *   dO          [B,H,n,64];  dstate optional [B,H,64,64] fp32: the gradient
+ *               that reaches the final state (NULL: 0).
+ *   dQ          out [B,H,n,64];  dK, dV out [B,Hk,n,64]: summed over the query
+ *               heads that share a key head, in fp32.
+ *   out_dstate  optional out [B,H,64,64] fp32: the initial state's gradient
+ *               (may be `dstate` itself).
+ * Workspace: ga_linear_backward_workspace_bytes.
+ */
+size_t ga_linear_backward_workspace_bytes(ga_shape_t s, int32_t Hk);
+int ga_linear_backward(ga_shape_t s, int32_t Hk, const void *Q, const void *K, const void *V, const void *dO,
+                       const float *log_decay, const int32_t *lengths, const float *state, const float *dstate,
+                       float scale, void *dQ, void *dK, void *dV, float *out_dstate, void *workspace,
+                       size_t workspace_bytes, void *stream);
+
+/*
+ * One token per sequence (s.n must be 1): ga_linear_attend's recurrence on
+ * kept states, in fp32 throughout.
+ *   state, out_state  [states,H,64,64] fp32; out_state may be `state` (an
+ *                     update in place).
+ *   slots             optional [B] int32: batch row b continues state
+ *                     slots[b]; NULL: row b has state b (states must be >= B).
+ *                     A row whose slot lies outside [0, states), or is that of
+ *                     an earlier row of the call, is padding: its output is
+ *                     zero and no state is touched for it.  States that no row
+ *                     names are not written.
+ */
+int ga_linear_step(ga_shape_t s, int32_t Hk, const void *Q, const void *K, const void *V, const float *log_decay,
+                   const int32_t *slots, int32_t states, const float *state, float scale, void *O, float *out_state,
+                   void *stream);
+
+/*
+ * Rotary positions with several axes on the queries and keys of an attention.
+ * The 64 features of a head form 32 pairs, (2i, 2i + 1) with GA_ROTARY_INTERLEAVED
+ * and (i, i + 32) without.  The first pairs[0] pairs belong to axis 0, the next
+ * pairs[1] to axis 1, and so on (a HOST array of `axes` values, each >= 1, at
+ * most 32 in sum); the pairs behind them are copied.  Pair m of an axis with p
+ * pairs is turned by the angle pos * base^(-m / p), or with GA_ROTARY_SHARED
+ * pair i (counted over all axes) by pos * base^(-i / 32).  GA_ROTARY_INVERSE
+ * turns by the negative angles: the inverse, and the gradient.
+ *   Q [B,H,n,64] and K [B,Hk,n,64] in s.dtype (K NULL: Q alone);
+ *   pos  [axes, pos_batches, n], pos_batches 1 or B: int32, or fp32 with
+ *        GA_ROTARY_FLOAT_POS (finite); negative positions are allowed, and
+ *        4-byte alignment is enough.
+ *   Qout, Kout  outputs; each may be its input itself.
+ * Angles are formed in fp64 and reduced to half a turn exactly, so far
+ * positions lose nothing; the turn is fp32, rounded once.  base > 0, finite.
+ */
+enum { GA_ROTARY_INTERLEAVED = 1, GA_ROTARY_SHARED = 2, GA_ROTARY_INVERSE = 4, GA_ROTARY_FLOAT_POS = 8 };
+#define GA_ROTARY_MAX_AXES 8
+int ga_rotary(ga_shape_t s, int32_t Hk, const void *Q, const void *K, const void *pos, int32_t pos_batches,
+              int32_t axes, const int32_t *pairs, double base, int32_t flags, void *Qout, void *Kout, void *stream);
+
+/*
+ * The norms after and before a block, fused with the block's gate and the
+ * residual's scale.  For every token, X the residual stream and F the block's
+ * output ([B,n,D] in dtype, 1 <= D <= 8192):
+ *   U = post-norm of F (F itself if post_w is NULL),
+ *   Y = residual_scale X + branch_scale gate * U,   H = pre-norm of Y,
+ *   norm(z) = w * z / sqrt(mean z^2 + eps) + c                     (GA_NORM_RMS)
+ *           = w * (z - mean z) / sqrt(var z + eps) + c             (GA_NORM_LAYER)
+ * The weights w, biases c (each optional) and gates are in dtype: w, c [D];
+ * gate [gate_batches, D] with gate_batches 0 (none), 1 or B.  H is formed from
+ * Y before its rounding.  F NULL: Y = residual_scale X (no post-norm, no gate):
+ * the norm before a first block.  Y and H are each optional, not both; H needs
+ * pre_w.  Sums are fp32, outputs rounded once; outputs must not overlap inputs.
+ */
+typedef enum { GA_NORM_RMS = 0, GA_NORM_LAYER = 1 } ga_norm_kind_t;
+typedef struct {
+    int32_t B, n, D, dtype; /* dtype: ga_dtype_t */
+    int32_t kind;           /* ga_norm_kind_t */
+    int32_t gate_batches;
+    float eps; /* > 0 */
+    float residual_scale, branch_scale;
+} ga_norm_t;
+int ga_norm_residual(ga_norm_t s, const void *X, const void *F, const void *post_w, const void *post_b,
+                     const void *gate, const void *pre_w, const void *pre_b, void *Y, void *H, void *stream);
+
+/*
+ * Gradient of ga_norm_residual.  dY, dH: the gradients that reach Y and H
+ * (each optional, not both; dH needs pre_w).  Outputs, each optional: dX, dF
+ * [B,n,D] in dtype; dpost_w, dpost_b, dpre_w, dpre_b [D] and dgate
+ * [gate_batches, D], fp32 sums over the tokens in a fixed order (a gradient of
+ * something the call does not have, e.g. dgate without a gate, is an error).
+ * Y and both norms are formed again from X and F.  Workspace:
+ * ga_norm_backward_workspace_bytes.
+ */
+size_t ga_norm_backward_workspace_bytes(ga_norm_t s);
+int ga_norm_residual_backward(ga_norm_t s, const void *X, const void *F, const void *post_w, const void *post_b,
+                              const void *gate, const void *pre_w, const void *pre_b, const void *dY, const void *dH,
+                              void *dX, void *dF, float *dpost_w, float *dpost_b, float *dgate, float *dpre_w,
+                              float *dpre_b, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
  * Per-kernel timing for measurement tools.  While enabled (per calling
  * thread), every kernel launch of this library is bracketed by a pair of
  * hipEvents recorded on the launch stream.  ga_timing_collect waits for the

@@ -14,7 +14,10 @@ SOURCES = [os.path.join(HERE, "csrc", "ga_abi.cpp"), os.path.join(HERE, "csrc", 
            os.path.join(HERE, "csrc", "ga_noalloc.hip"),
            os.path.join(HERE, "csrc", "ga_block.hip"),
            os.path.join(HERE, "csrc", "ga_merge.hip"),
-           os.path.join(HERE, "csrc", "ga_backward.hip")]
+           os.path.join(HERE, "csrc", "ga_backward.hip"),
+           os.path.join(HERE, "csrc", "ga_linear.hip"),
+           os.path.join(HERE, "csrc", "ga_rotary.hip"),
+           os.path.join(HERE, "csrc", "ga_norm.hip")]
 
 
 def hipcc() -> str:

@@ -65,6 +65,13 @@ int check_ptr(const void* p, const char* name, bool required) {
   return GA_OK;
 }
 
+// A pointer whose values are read one at a time (any slice of an array will do).
+int check_ptr_any(const void* p, const char* name, bool required) {
+  if (!p) return required ? fail(GA_ERR_INVALID_ARG, "%s is NULL", name) : GA_OK;
+  if (((uintptr_t)p & 3u) != 0) return fail(GA_ERR_INVALID_ARG, "%s is not 4-byte aligned", name);
+  return GA_OK;
+}
+
 int check_ws(const ga::Dims& d, void* ws, size_t bytes, ga::Workspace* w) {
   const size_t need = ga::workspace_layout(d, nullptr, nullptr);
   if (!ws) return fail(GA_ERR_WORKSPACE, "workspace is NULL (%zu bytes needed)", need);
@@ -210,6 +217,68 @@ size_t block_ws_layout(const ga_shape_t& s, int32_t N, void* base, void** qkvo, 
     ga::workspace_layout(d, w, (char*)base + 4 * t);
   }
   return 4 * t + rest;
+}
+
+// Shape checks of the linear attention and the rotary positions.
+int check_heads(const ga_shape_t& s, int32_t Hk, bool* empty) {
+  *empty = false;
+  if (s.dtype != GA_F32 && s.dtype != GA_BF16) return fail(GA_ERR_INVALID_ARG, "unknown dtype %d", s.dtype);
+  if (s.B < 0 || s.H < 0) return fail(GA_ERR_INVALID_ARG, "negative batch/head count (B=%d, H=%d)", s.B, s.H);
+  if (s.n < 1) return fail(GA_ERR_INVALID_ARG, "n must be >= 1 (got %d)", s.n);
+  if (s.d != ga::kD) return fail(GA_ERR_UNSUPPORTED, "only d = 64 is supported (got %d)", s.d);
+  if (s.H > 0 && (Hk < 1 || s.H % Hk != 0))
+    return fail(GA_ERR_INVALID_ARG, "the key heads must divide the query heads (H=%d, Hk=%d)", s.H, Hk);
+  if ((int64_t)s.B * s.H > 65535) return fail(GA_ERR_UNSUPPORTED, "B*H exceeds 65535");
+  if (s.n > (1 << 30)) return fail(GA_ERR_UNSUPPORTED, "n = %d too large", s.n);
+  *empty = s.B == 0 || s.H == 0;
+  return GA_OK;
+}
+
+ga::LinearDims linear_dims(const ga_shape_t& s, int32_t Hk) { return ga::LinearDims{s.B, s.H, Hk, s.n, s.dtype}; }
+
+// A workspace of `need` bytes (none needed: anything goes).
+int check_scratch(const void* ws, size_t bytes, size_t need) {
+  if (need == 0) return GA_OK;
+  if (!ws) return fail(GA_ERR_WORKSPACE, "workspace is NULL (%zu bytes needed)", need);
+  if (((uintptr_t)ws & 255u) != 0) return fail(GA_ERR_WORKSPACE, "workspace is not 256-byte aligned");
+  if (bytes < need) return fail(GA_ERR_WORKSPACE, "workspace has %zu bytes, %zu needed", bytes, need);
+  return GA_OK;
+}
+
+int check_norm(const ga_norm_t& s, bool* empty) {
+  *empty = false;
+  if (s.dtype != GA_F32 && s.dtype != GA_BF16) return fail(GA_ERR_INVALID_ARG, "unknown dtype %d", s.dtype);
+  if (s.B < 0) return fail(GA_ERR_INVALID_ARG, "negative batch count (B=%d)", s.B);
+  if (s.n < 1 || s.D < 1) return fail(GA_ERR_INVALID_ARG, "n and D must be >= 1 (n=%d, D=%d)", s.n, s.D);
+  if (s.kind != GA_NORM_RMS && s.kind != GA_NORM_LAYER) return fail(GA_ERR_INVALID_ARG, "unknown norm %d", s.kind);
+  if (s.gate_batches != 0 && s.gate_batches != 1 && s.gate_batches != s.B)
+    return fail(GA_ERR_INVALID_ARG, "gate_batches must be 0, 1 or B (got %d, B=%d)", s.gate_batches, s.B);
+  if (!(s.eps > 0.f) || !isfinite(s.eps)) return fail(GA_ERR_INVALID_ARG, "eps must be finite and > 0 (got %g)", s.eps);
+  if (!isfinite(s.residual_scale) || !isfinite(s.branch_scale))
+    return fail(GA_ERR_INVALID_ARG, "residual_scale and branch_scale must be finite");
+  if (s.D > ga::norm_max_width())
+    return fail(GA_ERR_UNSUPPORTED, "D = %d exceeds %d", s.D, ga::norm_max_width());
+  *empty = s.B == 0;
+  return GA_OK;
+}
+
+int check_norm_tensors(const ga_norm_t& s, const ga::NormTensors& t) {
+  GA_TRY(check_ptr(t.X, "X", true));
+  GA_TRY(check_ptr(t.F, "F", false));
+  GA_TRY(check_ptr(t.post_w, "post_w", false));
+  GA_TRY(check_ptr(t.post_b, "post_b", false));
+  GA_TRY(check_ptr(t.gate, "gate", s.gate_batches != 0));
+  GA_TRY(check_ptr(t.pre_w, "pre_w", false));
+  GA_TRY(check_ptr(t.pre_b, "pre_b", false));
+  if (t.gate && s.gate_batches == 0) return fail(GA_ERR_INVALID_ARG, "a gate needs gate_batches 1 or B");
+  if (!t.F && (t.post_w || t.gate)) return fail(GA_ERR_INVALID_ARG, "a post-norm or a gate needs F");
+  if (t.post_b && !t.post_w) return fail(GA_ERR_INVALID_ARG, "post_b needs post_w");
+  if (t.pre_b && !t.pre_w) return fail(GA_ERR_INVALID_ARG, "pre_b needs pre_w");
+  return GA_OK;
+}
+
+ga::NormDims norm_dims(const ga_norm_t& s) {
+  return ga::NormDims{s.B, s.n, s.D, s.dtype, s.kind, s.gate_batches, s.eps, s.residual_scale, s.branch_scale};
 }
 
 // ---------------------------------------------------------------- kernel timing
@@ -567,6 +636,184 @@ int ga_backward(ga_shape_t s, const void* Q, const void* dO, const int32_t* belo
   ga::backward_workspace_layout(d, &w, workspace);
   GA_LAUNCH(ga::launch_backward(d, Q, dO, belong, centroid, count, vsum, scale, dQ, dK, dV, w, (hipStream_t)stream),
             "backward launch");
+  return GA_OK;
+}
+
+size_t ga_linear_workspace_bytes(ga_shape_t s, int32_t Hk) {
+  bool empty;
+  const std::string keep = g_last_error;
+  const int rc = check_heads(s, Hk, &empty);
+  g_last_error = keep;
+  return rc != GA_OK || empty ? 0 : ga::linear_workspace(linear_dims(s, Hk));
+}
+
+int ga_linear_attend(ga_shape_t s, int32_t Hk, const void* Q, const void* K, const void* V, const float* log_decay,
+                     const int32_t* lengths, const float* state, float scale, void* O, float* out_state,
+                     void* workspace, size_t workspace_bytes, void* stream) {
+  bool empty;
+  GA_TRY(check_heads(s, Hk, &empty));
+  if (!isfinite(scale)) return fail(GA_ERR_INVALID_ARG, "scale must be finite");
+  if (empty) return GA_OK;
+  GA_TRY(check_ptr(Q, "Q", true));
+  GA_TRY(check_ptr(K, "K", true));
+  GA_TRY(check_ptr(V, "V", true));
+  GA_TRY(check_ptr_any(log_decay, "log_decay", true));
+  GA_TRY(check_ptr_any(lengths, "lengths", false));
+  GA_TRY(check_ptr(state, "state", false));
+  GA_TRY(check_ptr(O, "O", true));
+  GA_TRY(check_ptr(out_state, "out_state", false));
+  const ga::LinearDims d = linear_dims(s, Hk);
+  GA_TRY(check_scratch(workspace, workspace_bytes, ga::linear_workspace(d)));
+  GA_LAUNCH(ga::launch_linear(d, Q, K, V, log_decay, lengths, state, scale, O, out_state, workspace,
+                              (hipStream_t)stream), "linear-attention launch");
+  return GA_OK;
+}
+
+size_t ga_linear_backward_workspace_bytes(ga_shape_t s, int32_t Hk) {
+  bool empty;
+  const std::string keep = g_last_error;
+  const int rc = check_heads(s, Hk, &empty);
+  g_last_error = keep;
+  return rc != GA_OK || empty ? 0 : ga::linear_grad_workspace(linear_dims(s, Hk));
+}
+
+int ga_linear_backward(ga_shape_t s, int32_t Hk, const void* Q, const void* K, const void* V, const void* dO,
+                       const float* log_decay, const int32_t* lengths, const float* state, const float* dstate,
+                       float scale, void* dQ, void* dK, void* dV, float* out_dstate, void* workspace,
+                       size_t workspace_bytes, void* stream) {
+  bool empty;
+  GA_TRY(check_heads(s, Hk, &empty));
+  if (!isfinite(scale)) return fail(GA_ERR_INVALID_ARG, "scale must be finite");
+  if (empty) return GA_OK;
+  GA_TRY(check_ptr(Q, "Q", true));
+  GA_TRY(check_ptr(K, "K", true));
+  GA_TRY(check_ptr(V, "V", true));
+  GA_TRY(check_ptr(dO, "dO", true));
+  GA_TRY(check_ptr_any(log_decay, "log_decay", true));
+  GA_TRY(check_ptr_any(lengths, "lengths", false));
+  GA_TRY(check_ptr(state, "state", false));
+  GA_TRY(check_ptr(dstate, "dstate", false));
+  GA_TRY(check_ptr(dQ, "dQ", true));
+  GA_TRY(check_ptr(dK, "dK", true));
+  GA_TRY(check_ptr(dV, "dV", true));
+  GA_TRY(check_ptr(out_dstate, "out_dstate", false));
+  const ga::LinearDims d = linear_dims(s, Hk);
+  GA_TRY(check_scratch(workspace, workspace_bytes, ga::linear_grad_workspace(d)));
+  GA_LAUNCH(ga::launch_linear_grad(d, Q, K, V, dO, log_decay, lengths, state, dstate, scale, dQ, dK, dV, out_dstate,
+                                   workspace, (hipStream_t)stream), "linear-attention gradient launch");
+  return GA_OK;
+}
+
+int ga_linear_step(ga_shape_t s, int32_t Hk, const void* Q, const void* K, const void* V, const float* log_decay,
+                   const int32_t* slots, int32_t states, const float* state, float scale, void* O, float* out_state,
+                   void* stream) {
+  bool empty;
+  GA_TRY(check_heads(s, Hk, &empty));
+  if (s.n != 1) return fail(GA_ERR_INVALID_ARG, "a step takes one token per sequence (n=%d)", s.n);
+  if (!isfinite(scale)) return fail(GA_ERR_INVALID_ARG, "scale must be finite");
+  if (states < 0 || (!slots && states < s.B))
+    return fail(GA_ERR_INVALID_ARG, "%d states for %d sequences", states, s.B);
+  if (empty) return GA_OK;
+  GA_TRY(check_ptr(Q, "Q", true));
+  GA_TRY(check_ptr(K, "K", true));
+  GA_TRY(check_ptr(V, "V", true));
+  GA_TRY(check_ptr_any(log_decay, "log_decay", true));
+  GA_TRY(check_ptr_any(slots, "slots", false));
+  GA_TRY(check_ptr(state, "state", states > 0));
+  GA_TRY(check_ptr(O, "O", true));
+  GA_TRY(check_ptr(out_state, "out_state", states > 0));
+  GA_LAUNCH(ga::launch_linear_step(linear_dims(s, Hk), Q, K, V, log_decay, slots, states, state, scale, O, out_state,
+                                   (hipStream_t)stream), "linear-attention step launch");
+  return GA_OK;
+}
+
+int ga_rotary(ga_shape_t s, int32_t Hk, const void* Q, const void* K, const void* pos, int32_t pos_batches,
+              int32_t axes, const int32_t* pairs, double base, int32_t flags, void* Qout, void* Kout, void* stream) {
+  bool empty;
+  GA_TRY(check_heads(s, K ? Hk : s.H, &empty));
+  if (pos_batches != 1 && pos_batches != s.B)
+    return fail(GA_ERR_INVALID_ARG, "pos_batches must be 1 or B (got %d, B=%d)", pos_batches, s.B);
+  if (axes < 1 || axes > GA_ROTARY_MAX_AXES || !pairs)
+    return fail(GA_ERR_INVALID_ARG, "1 to %d axes with their pairs are needed (axes=%d)", GA_ROTARY_MAX_AXES, axes);
+  if (!(base > 0.0) || !isfinite(base)) return fail(GA_ERR_INVALID_ARG, "base must be finite and > 0 (got %g)", base);
+  if (flags & ~15) return fail(GA_ERR_INVALID_ARG, "unknown flags 0x%x", (unsigned)flags);
+  ga::RotaryPlan plan{};
+  plan.pos_batches = pos_batches;
+  plan.pos_float = (flags & GA_ROTARY_FLOAT_POS) != 0;
+  const double turn = (flags & GA_ROTARY_INVERSE ? -1.0 : 1.0) / (2.0 * M_PI);
+  int i = 0;
+  for (int a = 0; a < axes; ++a) {
+    if (pairs[a] < 1 || pairs[a] > 32 - i)
+      return fail(GA_ERR_INVALID_ARG, "each axis needs at least one pair, at most 32 in sum (axis %d: %d)", a, pairs[a]);
+    for (int m = 0; m < pairs[a]; ++m, ++i) {
+      const double e = flags & GA_ROTARY_SHARED ? -(double)i / 32.0 : -(double)m / pairs[a];
+      plan.turns[i] = turn * pow(base, e);
+      plan.axis[i] = (uint8_t)a;
+    }
+  }
+  if (empty) return GA_OK;
+  GA_TRY(check_ptr(Q, "Q", true));
+  GA_TRY(check_ptr(K, "K", false));
+  GA_TRY(check_ptr_any(pos, "pos", true));
+  GA_TRY(check_ptr(Qout, "Qout", true));
+  GA_TRY(check_ptr(Kout, "Kout", K != nullptr));
+  GA_LAUNCH(ga::launch_rotary(s.dtype, s.B, s.H, K ? Hk : 0, s.n, Q, K, pos, plan, (flags & GA_ROTARY_INTERLEAVED) != 0,
+                              Qout, Kout, (hipStream_t)stream), "rotary launch");
+  return GA_OK;
+}
+
+int ga_norm_residual(ga_norm_t s, const void* X, const void* F, const void* post_w, const void* post_b,
+                     const void* gate, const void* pre_w, const void* pre_b, void* Y, void* H, void* stream) {
+  bool empty;
+  GA_TRY(check_norm(s, &empty));
+  if (empty) return GA_OK;
+  const ga::NormTensors t{X, F, post_w, post_b, gate, pre_w, pre_b};
+  GA_TRY(check_norm_tensors(s, t));
+  GA_TRY(check_ptr(Y, "Y", false));
+  GA_TRY(check_ptr(H, "H", false));
+  if (!Y && !H) return fail(GA_ERR_INVALID_ARG, "neither Y nor H is asked for");
+  if (H && !pre_w) return fail(GA_ERR_INVALID_ARG, "H needs pre_w");
+  GA_LAUNCH(ga::launch_norm(norm_dims(s), t, Y, H, (hipStream_t)stream), "norm launch");
+  return GA_OK;
+}
+
+size_t ga_norm_backward_workspace_bytes(ga_norm_t s) {
+  bool empty;
+  const std::string keep = g_last_error;
+  const int rc = check_norm(s, &empty);
+  g_last_error = keep;
+  return rc != GA_OK || empty ? 0 : ga::norm_grad_workspace(norm_dims(s));
+}
+
+int ga_norm_residual_backward(ga_norm_t s, const void* X, const void* F, const void* post_w, const void* post_b,
+                              const void* gate, const void* pre_w, const void* pre_b, const void* dY, const void* dH,
+                              void* dX, void* dF, float* dpost_w, float* dpost_b, float* dgate, float* dpre_w,
+                              float* dpre_b, void* workspace, size_t workspace_bytes, void* stream) {
+  bool empty;
+  GA_TRY(check_norm(s, &empty));
+  if (empty) return GA_OK;
+  const ga::NormTensors t{X, F, post_w, post_b, gate, pre_w, pre_b};
+  GA_TRY(check_norm_tensors(s, t));
+  GA_TRY(check_ptr(dY, "dY", false));
+  GA_TRY(check_ptr(dH, "dH", false));
+  if (!dY && !dH) return fail(GA_ERR_INVALID_ARG, "neither dY nor dH is given");
+  if (dH && !pre_w) return fail(GA_ERR_INVALID_ARG, "dH needs pre_w");
+  GA_TRY(check_ptr(dX, "dX", false));
+  GA_TRY(check_ptr(dF, "dF", false));
+  float* const out[5] = {dpost_w, dpost_b, dpre_w, dpre_b, dgate};
+  const char* const names[5] = {"dpost_w", "dpost_b", "dpre_w", "dpre_b", "dgate"};
+  const bool has[5] = {post_w != nullptr, post_b != nullptr, dH != nullptr, dH && pre_b, gate != nullptr};
+  bool any = dX || dF;
+  for (int i = 0; i < 5; ++i) {
+    GA_TRY(check_ptr(out[i], names[i], false));
+    if (out[i] && !has[i]) return fail(GA_ERR_INVALID_ARG, "%s is asked for, but the call has nothing it belongs to", names[i]);
+    any = any || out[i];
+  }
+  if (dF && !F) return fail(GA_ERR_INVALID_ARG, "dF needs F");
+  if (!any) return fail(GA_ERR_INVALID_ARG, "no gradient is asked for");
+  const ga::NormDims d = norm_dims(s);
+  GA_TRY(check_scratch(workspace, workspace_bytes, ga::norm_grad_workspace(d)));
+  GA_LAUNCH(ga::launch_norm_grad(d, t, dY, dH, dX, dF, out, workspace, (hipStream_t)stream), "norm gradient launch");
   return GA_OK;
 }
 

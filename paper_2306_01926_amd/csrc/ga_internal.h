@@ -187,4 +187,47 @@ hipError_t launch_backward(const Dims& d, const void* Q, const void* dO, const i
                            const float* centroid, const int32_t* count, const float* vsum, float scale, void* dQ,
                            void* dK, void* dV, const BackwardWorkspace& w, hipStream_t st);
 
+// Linear attention with a decay for each head (ga_linear.hip).
+struct LinearDims {
+  int B, H, Hk, n, dtype;  // dtype: 0 fp32, 1 bf16
+};
+size_t linear_workspace(const LinearDims& d);
+hipError_t launch_linear(const LinearDims& d, const void* Q, const void* K, const void* V, const float* log_decay,
+                         const int32_t* lengths, const float* state, float scale, void* O, float* state_out, void* ws,
+                         hipStream_t st);
+size_t linear_grad_workspace(const LinearDims& d);
+hipError_t launch_linear_grad(const LinearDims& d, const void* Q, const void* K, const void* V, const void* dO,
+                              const float* log_decay, const int32_t* lengths, const float* state, const float* dstate,
+                              float scale, void* dQ, void* dK, void* dV, float* dstate_out, void* ws, hipStream_t st);
+hipError_t launch_linear_step(const LinearDims& d, const void* Q, const void* K, const void* V, const float* log_decay,
+                              const int32_t* slots, int states, const float* state, float scale, void* O,
+                              float* state_out, hipStream_t st);
+
+// Rotary positions (ga_rotary.hip): each pair's axis and its turns per unit of
+// position (negative for the inverse; 0 for a pair that is copied).
+struct RotaryPlan {
+  double turns[32];
+  uint8_t axis[32];
+  int pos_batches;
+  bool pos_float;
+};
+hipError_t launch_rotary(int dtype, int B, int H, int Hk, int n, const void* Q, const void* K, const void* pos,
+                         const RotaryPlan& plan, bool interleaved, void* Qo, void* Ko, hipStream_t st);
+
+// Norms around a block (ga_norm.hip).
+struct NormDims {
+  int B, n, W, dtype;
+  int layer, gate_batches;
+  float eps, a, b;  // a: the residual's scale, b: the branch's
+};
+struct NormTensors {
+  const void *X, *F, *post_w, *post_b, *gate, *pre_w, *pre_b;
+};
+int norm_max_width();
+hipError_t launch_norm(const NormDims& d, const NormTensors& t, void* Y, void* H, hipStream_t st);
+size_t norm_grad_workspace(const NormDims& d);
+// out: dpost_w, dpost_b, dpre_w, dpre_b, dgate
+hipError_t launch_norm_grad(const NormDims& d, const NormTensors& t, const void* dY, const void* dH, void* dX,
+                            void* dF, float* const out[5], void* ws, hipStream_t st);
+
 }  // namespace ga

@@ -1,0 +1,485 @@
+// gfx950 (MI355X) norms around a block, fused with its gate and the residual's
+// scale, and their gradient.
+//
+// For every token (row of W features), x the residual stream, f the block's
+// output:
+//   u = post-norm of f (f itself without one),
+//   y = a x + b g * u          (a, b scalars, g a gate per feature),
+//   h = pre-norm of y          (the next block's input),
+//   norm(z) = w * (z - mean z) / sqrt(var z + eps) + c     (layer)
+//           = w * z / sqrt(mean z^2 + eps) + c             (rms).
+// Gradient, with zn the normalised row, r its 1 / sqrt(...) and P the
+// projection P(d) = r (d - zn mean(d zn) [- mean d for layer]):
+//   D  = dy + P_y(w_pre dh),   dx = a D,
+//   df = P_f(w_post b g D),    dw_post = sum b g D fn,  dc_post = sum b g D,
+//   dg = sum b u D,            dw_pre  = sum dh yn,     dc_pre  = sum dh.
+// The gradient forms y and both norms again from x and f (the same bytes as
+// reading a stored y), so nothing is kept from the forward pass.
+//
+// Both are bound by HBM: 4 rows of W values moved per token forward (x, f in,
+// y, h out), 6 backward.  A row lives in the registers of TPR threads, eight
+// consecutive features each, so it is read once; the variance is the mean
+// square about the mean, formed from those registers (two sums), all in fp32.
+// One wave holds a row of up to 512 features and reduces by lane exchanges
+// only.  Parameter gradients are summed over a workgroup's rows in registers,
+// its teams are added in LDS, and a second launch adds the workgroups' rows in
+// ascending order: no atomics, the same bits on every run.
+#include <hip/hip_runtime.h>
+
+#include <float.h>
+#include <stdint.h>
+
+#include "ga_internal.h"
+
+namespace ga {
+namespace {
+
+#include "ga_device.h"
+
+constexpr int kE = 8;  // features per thread
+
+// Eight features of one row from column c (beyond W: zeros).  VEC: W is a
+// multiple of eight, so every group of eight is whole and 16-byte aligned.
+template <class DT, bool VEC>
+__device__ __forceinline__ void load8(const typename DT::T* p, int c, int W, float (&v)[kE]) {
+  if constexpr (VEC) {
+    if (c >= W) {
+#pragma unroll
+      for (int e = 0; e < kE; ++e) v[e] = 0.f;
+    } else if constexpr (DT::kBits == 16) {
+      const u32x4 w = *(const u32x4*)(p + c);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        v[2 * e] = bf16_to_f32(w[e] & 0xffffu);
+        v[2 * e + 1] = bf16_to_f32(w[e] >> 16);
+      }
+    } else {
+      const float4 a = *(const float4*)(p + c), b = *(const float4*)(p + c + 4);
+      v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < kE; ++e) v[e] = c + e < W ? DT::load(p, c + e) : 0.f;
+  }
+}
+
+// The outputs are rounded once, to nearest even (bf16), here.
+template <class DT, bool VEC>
+__device__ __forceinline__ void store8(typename DT::T* p, int c, int W, const float (&v)[kE]) {
+  if constexpr (VEC) {
+    if (c >= W) return;
+    if constexpr (DT::kBits == 16) {
+      u32x4 w;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) w[e] = pack_bf16x2(v[2 * e], v[2 * e + 1]);
+      *(u32x4*)(p + c) = w;
+    } else {
+      *(float4*)(p + c) = make_float4(v[0], v[1], v[2], v[3]);
+      *(float4*)(p + c + 4) = make_float4(v[4], v[5], v[6], v[7]);
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < kE; ++e) {
+      if (c + e >= W) continue;
+      if constexpr (DT::kBits == 16)
+        p[c + e] = (uint16_t)(pack_bf16x2(v[e], 0.f) & 0xffffu);
+      else
+        p[c + e] = v[e];
+    }
+  }
+}
+
+// Sums of two values over the TPR threads of a team, in every thread of it.
+// Teams of more than a wave exchange through red[16], one entry per wave.
+// The calls inside one row's work have a red each, and rows alternate between
+// two sets of them: whoever writes an entry again has passed the barrier of a
+// later call (in the next row at the latest), before which every wave had read
+// it.
+template <int TPR>
+__device__ __forceinline__ float2 team_sum(float a, float b, float2* red) {
+#pragma unroll
+  for (int m = 1; m < (TPR < 64 ? TPR : 64); m <<= 1) {
+    a += __shfl_xor(a, m);
+    b += __shfl_xor(b, m);
+  }
+  if constexpr (TPR > 64) {
+    constexpr int kW = TPR / 64;  // waves per team
+    const int wave = threadIdx.x >> 6, first = wave / kW * kW;
+    if ((threadIdx.x & 63) == 0) red[wave] = make_float2(a, b);
+    __syncthreads();
+    a = b = 0.f;
+#pragma unroll
+    for (int w = 0; w < kW; ++w) {
+      const float2 r = red[first + w];
+      a += r.x;
+      b += r.y;
+    }
+  }
+  return make_float2(a, b);
+}
+
+constexpr int wg_threads(int TPR) { return TPR < 256 ? 256 : TPR; }
+
+// z -> zn = (z - mean) r in place; returns r.  red: a buffer of this call's own.
+template <int TPR>
+__device__ __forceinline__ float normalise(float (&z)[kE], int c, int W, float invW, bool layer, float eps,
+                                           float2 (*red)[16]) {
+  if (layer) {
+    float s = 0.f;
+#pragma unroll
+    for (int e = 0; e < kE; ++e) s += z[e];
+    const float mean = team_sum<TPR>(s, 0.f, red[0]).x * invW;
+#pragma unroll
+    for (int e = 0; e < kE; ++e) z[e] = c + e < W ? z[e] - mean : 0.f;
+  }
+  float q = 0.f;
+#pragma unroll
+  for (int e = 0; e < kE; ++e) q = fmaf(z[e], z[e], q);
+  const float r = 1.0f / sqrtf(team_sum<TPR>(q, 0.f, red[1]).x * invW + eps);
+#pragma unroll
+  for (int e = 0; e < kE; ++e) z[e] *= r;
+  return r;
+}
+
+// d -> P(d) in place (see the head of the file).
+template <int TPR>
+__device__ __forceinline__ void project(float (&d)[kE], const float (&zn)[kE], float r, int c, int W, float invW,
+                                        bool layer, float2* red) {
+  float s = 0.f, t = 0.f;
+#pragma unroll
+  for (int e = 0; e < kE; ++e) {
+    s = fmaf(d[e], zn[e], s);
+    t += d[e];
+  }
+  const float2 m = team_sum<TPR>(s, t, red);
+  const float mz = m.x * invW, md = layer ? m.y * invW : 0.f;
+#pragma unroll
+  for (int e = 0; e < kE; ++e) d[e] = c + e < W ? r * (d[e] - fmaf(zn[e], mz, md)) : 0.f;
+}
+
+template <class DT>
+struct NormArgs {
+  using T = typename DT::T;
+  const T *X, *F, *post_w, *post_b, *gate, *pre_w, *pre_b;
+  int64_t rows;      // tokens
+  int n, W;          // tokens per batch, features
+  int gate_batches;  // 0: no gate, 1: one for all tokens, B: one per batch
+  float invW, eps, a, b;
+  bool layer;
+};
+
+template <class DT, int TPR, bool VEC>
+__global__ __launch_bounds__(wg_threads(TPR)) void k_norm(NormArgs<DT> A, typename DT::T* __restrict__ Y,
+                                                          typename DT::T* __restrict__ Ho) {
+  __shared__ float2 reds[2][4][16];
+  constexpr int kTeams = wg_threads(TPR) / TPR;
+  const int team = threadIdx.x / TPR, c = (threadIdx.x % TPR) * kE, W = A.W;
+  float pw[kE], pb[kE], gt[kE], qw[kE], qb[kE];
+  if (A.post_w) load8<DT, VEC>(A.post_w, c, W, pw);
+  if (A.post_b) load8<DT, VEC>(A.post_b, c, W, pb);
+  if (A.gate_batches == 1) load8<DT, VEC>(A.gate, c, W, gt);
+  if (Ho) load8<DT, VEC>(A.pre_w, c, W, qw);
+  if (Ho && A.pre_b) load8<DT, VEC>(A.pre_b, c, W, qb);
+  int parity = 0;
+  // every team makes the same number of turns (barriers inside)
+  for (int64_t row0 = (int64_t)blockIdx.x * kTeams; row0 < A.rows; row0 += (int64_t)gridDim.x * kTeams) {
+    float2(*red)[16] = reds[parity];
+    parity ^= 1;
+    const bool live = row0 + team < A.rows;
+    const int64_t row = live ? row0 + team : A.rows - 1;
+    float y[kE], u[kE];
+    load8<DT, VEC>(A.X + row * W, c, W, y);
+    if (A.F) load8<DT, VEC>(A.F + row * W, c, W, u);
+    if (A.gate_batches > 1) load8<DT, VEC>(A.gate + row / A.n * W, c, W, gt);
+#pragma unroll
+    for (int e = 0; e < kE; ++e) y[e] *= A.a;
+    if (A.F) {
+      if (A.post_w) {
+        normalise<TPR>(u, c, W, A.invW, A.layer, A.eps, red);
+#pragma unroll
+        for (int e = 0; e < kE; ++e) u[e] = fmaf(u[e], pw[e], A.post_b ? pb[e] : 0.f);
+      }
+#pragma unroll
+      for (int e = 0; e < kE; ++e) y[e] = fmaf(A.gate_batches ? A.b * gt[e] : A.b, u[e], y[e]);
+    }
+    if (Y && live) store8<DT, VEC>(Y + row * W, c, W, y);
+    if (Ho) {
+      normalise<TPR>(y, c, W, A.invW, A.layer, A.eps, red + 2);
+#pragma unroll
+      for (int e = 0; e < kE; ++e) y[e] = fmaf(y[e], qw[e], A.pre_b ? qb[e] : 0.f);
+      if (live) store8<DT, VEC>(Ho + row * W, c, W, y);
+    }
+  }
+}
+
+// Rows of one batch group are spread over `split` workgroups, or a workgroup
+// takes `each` whole groups (split == 1).  part: [gridDim.x][4][W] sums of
+// dpost_w, dpost_b, dpre_w, dpre_b; gpart: [groups][split][W] sums of dgate.
+struct NormParts {
+  float *part, *gpart;
+  int groups, split, each;
+  int64_t group_rows;
+};
+
+template <int TPR>
+__device__ __forceinline__ void team_store(const float (&v)[kE], float* buf, float* dst, int W) {
+  constexpr int kT = wg_threads(TPR), kTeams = kT / TPR;
+  __syncthreads();
+#pragma unroll
+  for (int e = 0; e < kE; ++e) buf[(threadIdx.x / TPR) * (TPR * kE) + (threadIdx.x % TPR) * kE + e] = v[e];
+  __syncthreads();
+  for (int col = threadIdx.x; col < W; col += kT) {
+    float s = 0.f;
+#pragma unroll
+    for (int t = 0; t < kTeams; ++t) s += buf[t * (TPR * kE) + col];
+    dst[col] = s;
+  }
+}
+
+template <class DT, int TPR, bool VEC>
+__global__ __launch_bounds__(wg_threads(TPR)) void k_norm_grad(NormArgs<DT> A, const typename DT::T* __restrict__ dY,
+                                                               const typename DT::T* __restrict__ dH,
+                                                               typename DT::T* __restrict__ dX,
+                                                               typename DT::T* __restrict__ dF, NormParts P) {
+  constexpr int kT = wg_threads(TPR), kTeams = kT / TPR;
+  __shared__ float2 reds[2][6][16];
+  __shared__ float buf[kT * kE];
+  const int team = threadIdx.x / TPR, c = (threadIdx.x % TPR) * kE, W = A.W;
+  float pw[kE], pb[kE], gt[kE], qw[kE];
+  if (A.post_w) load8<DT, VEC>(A.post_w, c, W, pw);
+  if (A.post_b) load8<DT, VEC>(A.post_b, c, W, pb);
+  if (dH) load8<DT, VEC>(A.pre_w, c, W, qw);
+  float spw[kE], spb[kE], sqw[kE], sqb[kE], sg[kE];
+#pragma unroll
+  for (int e = 0; e < kE; ++e) spw[e] = spb[e] = sqw[e] = sqb[e] = 0.f;
+
+  int parity = 0;
+  for (int i = 0; i < P.each; ++i) {
+    const int grp = P.split > 1 ? blockIdx.x / P.split : blockIdx.x * P.each + i;
+    if (grp >= P.groups) break;  // the same for every thread
+    const int share = P.split > 1 ? blockIdx.x % P.split : 0;
+#pragma unroll
+    for (int e = 0; e < kE; ++e) sg[e] = 0.f;
+    if (A.gate_batches) load8<DT, VEC>(A.gate + (A.gate_batches > 1 ? (int64_t)grp * W : 0), c, W, gt);
+    for (int64_t r0 = (int64_t)share * kTeams; r0 < P.group_rows; r0 += (int64_t)P.split * kTeams) {
+      float2(*red)[16] = reds[parity];
+      parity ^= 1;
+      const bool live = r0 + team < P.group_rows;
+      const int64_t row = grp * P.group_rows + (live ? r0 + team : P.group_rows - 1);
+      float y[kE], u[kE], fn[kE], d[kE], dh[kE], rf = 0.f;
+      load8<DT, VEC>(A.X + row * W, c, W, y);
+      if (A.F) load8<DT, VEC>(A.F + row * W, c, W, fn);
+      if (dY) {
+        load8<DT, VEC>(dY + row * W, c, W, d);
+      } else {
+#pragma unroll
+        for (int e = 0; e < kE; ++e) d[e] = 0.f;
+      }
+      if (dH) load8<DT, VEC>(dH + row * W, c, W, dh);
+#pragma unroll
+      for (int e = 0; e < kE; ++e) y[e] *= A.a;
+      if (A.F) {
+        if (A.post_w) {
+          rf = normalise<TPR>(fn, c, W, A.invW, A.layer, A.eps, red);
+#pragma unroll
+          for (int e = 0; e < kE; ++e) u[e] = fmaf(fn[e], pw[e], A.post_b ? pb[e] : 0.f);
+        } else {
+#pragma unroll
+          for (int e = 0; e < kE; ++e) u[e] = fn[e];
+        }
+#pragma unroll
+        for (int e = 0; e < kE; ++e) y[e] = fmaf(A.gate_batches ? A.b * gt[e] : A.b, u[e], y[e]);
+      }
+      if (dH) {
+        const float rh = normalise<TPR>(y, c, W, A.invW, A.layer, A.eps, red + 2);
+        float dn[kE];
+#pragma unroll
+        for (int e = 0; e < kE; ++e) {
+          if (live) {
+            sqw[e] = fmaf(dh[e], y[e], sqw[e]);
+            sqb[e] += dh[e];
+          }
+          dn[e] = dh[e] * qw[e];
+          if (c + e >= W) dn[e] = 0.f;
+        }
+        project<TPR>(dn, y, rh, c, W, A.invW, A.layer, red[4]);
+#pragma unroll
+        for (int e = 0; e < kE; ++e) d[e] += dn[e];
+      }
+      if (A.F) {
+        float du[kE];
+#pragma unroll
+        for (int e = 0; e < kE; ++e) {
+          const float bd = A.b * d[e];
+          if (live) sg[e] = fmaf(bd, u[e], sg[e]);
+          du[e] = A.gate_batches ? bd * gt[e] : bd;
+        }
+        if (A.post_w) {
+#pragma unroll
+          for (int e = 0; e < kE; ++e) {
+            if (live) {
+              spw[e] = fmaf(du[e], fn[e], spw[e]);
+              spb[e] += du[e];
+            }
+            du[e] *= pw[e];
+            if (c + e >= W) du[e] = 0.f;
+          }
+          project<TPR>(du, fn, rf, c, W, A.invW, A.layer, red[5]);
+        }
+        if (dF && live) store8<DT, VEC>(dF + row * W, c, W, du);
+      }
+      if (dX && live) {
+#pragma unroll
+        for (int e = 0; e < kE; ++e) d[e] *= A.a;
+        store8<DT, VEC>(dX + row * W, c, W, d);
+      }
+    }
+    if (P.gpart) team_store<TPR>(sg, buf, P.gpart + ((int64_t)grp * P.split + share) * W, W);
+  }
+  if (P.part) {
+    float* dst = P.part + (int64_t)blockIdx.x * 4 * W;
+    if (A.post_w) {
+      team_store<TPR>(spw, buf, dst, W);
+      team_store<TPR>(spb, buf, dst + W, W);
+    }
+    if (dH) {
+      team_store<TPR>(sqw, buf, dst + 2 * W, W);
+      team_store<TPR>(sqb, buf, dst + 3 * W, W);
+    }
+  }
+}
+
+// out[g][col] = sum over parts p of src[(g parts + p) stride + col], in
+// ascending order within each of 16 interleaved shares.  grid (ceil(W / 16),
+// outputs, groups of the gate).
+struct NormOuts {
+  float* out[5];
+};
+__global__ __launch_bounds__(256) void k_norm_params(const float* __restrict__ part, const float* __restrict__ gpart,
+                                                     int wgs, int groups, int split, int W, NormOuts O) {
+  __shared__ float buf[16][17];
+  const int which = blockIdx.y;
+  float* out = O.out[which];
+  if (!out || (which != 4 && blockIdx.z > 0)) return;
+  const float* src = which == 4 ? gpart + (int64_t)blockIdx.z * split * W : part + (int64_t)which * W;
+  const int64_t stride = which == 4 ? W : 4 * (int64_t)W;
+  const int count = which == 4 ? split : wgs;
+  const int cl = threadIdx.x & 15, s = threadIdx.x >> 4, col = blockIdx.x * 16 + cl;
+  float v = 0.f;
+  if (col < W)
+    for (int p = s; p < count; p += 16) v += src[p * stride + col];
+  buf[s][cl] = v;
+  __syncthreads();
+  if (s == 0 && col < W) {
+    float t = 0.f;
+#pragma unroll
+    for (int k = 0; k < 16; ++k) t += buf[k][cl];
+    out[(which == 4 ? (int64_t)blockIdx.z * W : 0) + col] = t;
+  }
+}
+
+int threads_per_row(int W) {
+  int t = 8;
+  while (t * kE < W) t *= 2;
+  return t;
+}
+
+// The gradient's grouping of rows into workgroups.  One workgroup's sums cost
+// a pass over its rows' registers at the end, so there are only as many as
+// fill the compute units twice; a gate per batch keeps a workgroup inside one
+// batch, or gives it several whole ones where batches are many.
+constexpr int kNormWgs = 512;
+NormParts parts_of(const NormDims& d) {
+  NormParts p{};
+  p.groups = d.gate_batches > 1 ? d.gate_batches : 1;
+  p.group_rows = d.gate_batches > 1 ? d.n : (int64_t)d.B * d.n;
+  const int tpr = threads_per_row(d.W), teams = wg_threads(tpr) / tpr;
+  const int64_t most = (p.group_rows + teams - 1) / teams;
+  int64_t split = kNormWgs / p.groups;
+  p.split = (int)(split < 1 ? 1 : (split > most ? most : split));
+  p.each = p.split > 1 ? 1 : (p.groups + kNormWgs - 1) / kNormWgs;
+  return p;
+}
+int wgs_of(const NormParts& p) { return p.split > 1 ? p.groups * p.split : (p.groups + p.each - 1) / p.each; }
+
+template <class DT>
+NormArgs<DT> args_of(const NormDims& d, const NormTensors& t) {
+  using T = typename DT::T;
+  return NormArgs<DT>{(const T*)t.X,    (const T*)t.F,     (const T*)t.post_w, (const T*)t.post_b, (const T*)t.gate,
+                      (const T*)t.pre_w, (const T*)t.pre_b, (int64_t)d.B * d.n, d.n,                d.W,
+                      d.gate_batches,   1.0f / (float)d.W, d.eps,              d.a,                d.b,
+                      d.layer != 0};
+}
+
+#define GA_NORM_TPR(DT, VEC, CALL) \
+  switch (threads_per_row(d.W)) {  \
+    case 8: CALL(DT, 8, VEC); break;     \
+    case 16: CALL(DT, 16, VEC); break;   \
+    case 32: CALL(DT, 32, VEC); break;   \
+    case 64: CALL(DT, 64, VEC); break;   \
+    case 128: CALL(DT, 128, VEC); break; \
+    case 256: CALL(DT, 256, VEC); break; \
+    case 512: CALL(DT, 512, VEC); break; \
+    default: CALL(DT, 1024, VEC); break; \
+  }
+#define GA_NORM_ALL(CALL)                        \
+  if (d.dtype == 1 && d.W % kE == 0) {           \
+    GA_NORM_TPR(BF16, true, CALL)                \
+  } else if (d.dtype == 1) {                     \
+    GA_NORM_TPR(BF16, false, CALL)               \
+  } else if (d.W % kE == 0) {                    \
+    GA_NORM_TPR(F32, true, CALL)                 \
+  } else {                                       \
+    GA_NORM_TPR(F32, false, CALL)                \
+  }
+
+}  // namespace
+
+int norm_max_width() { return 1024 * kE; }
+
+hipError_t launch_norm(const NormDims& d, const NormTensors& t, void* Y, void* H, hipStream_t st) {
+  const int tpr = threads_per_row(d.W), teams = wg_threads(tpr) / tpr;
+  const int64_t rows = (int64_t)d.B * d.n, wgs = (rows + teams - 1) / teams;
+  const unsigned grid = (unsigned)(wgs < 4096 ? wgs : 4096);
+  TimedLaunch tl("norm", st);
+#define GA_CALL(DT, TPR, VEC)                                                                               \
+  hipLaunchKernelGGL((k_norm<DT, TPR, VEC>), dim3(grid), dim3(wg_threads(TPR)), 0, st, args_of<DT>(d, t),    \
+                     (typename DT::T*)Y, (typename DT::T*)H)
+  GA_NORM_ALL(GA_CALL)
+#undef GA_CALL
+  return hipGetLastError();
+}
+
+size_t norm_grad_workspace(const NormDims& d) {
+  const NormParts p = parts_of(d);
+  return ((size_t)wgs_of(p) * 4 + (size_t)p.groups * p.split) * d.W * 4;
+}
+
+hipError_t launch_norm_grad(const NormDims& d, const NormTensors& t, const void* dY, const void* dH, void* dX,
+                            void* dF, float* const out[5], void* ws, hipStream_t st) {
+  NormParts p = parts_of(d);
+  const int wgs = wgs_of(p);
+  const bool params = out[0] || out[1] || out[2] || out[3];
+  p.part = params ? (float*)ws : nullptr;
+  // a group of one share is the result itself
+  p.gpart = !out[4] ? nullptr : (p.split == 1 ? out[4] : (float*)ws + (size_t)wgs * 4 * d.W);
+  {
+    TimedLaunch tl("norm_grad", st);
+#define GA_CALL(DT, TPR, VEC)                                                                                     \
+  hipLaunchKernelGGL((k_norm_grad<DT, TPR, VEC>), dim3((unsigned)wgs), dim3(wg_threads(TPR)), 0, st,               \
+                     args_of<DT>(d, t), (const typename DT::T*)dY, (const typename DT::T*)dH, (typename DT::T*)dX, \
+                     (typename DT::T*)dF, p)
+    GA_NORM_ALL(GA_CALL)
+#undef GA_CALL
+  }
+  const bool gate = out[4] && p.split > 1;
+  if (params || gate) {
+    TimedLaunch tl("norm_params", st);
+    NormOuts o{{out[0], out[1], out[2], out[3], gate ? out[4] : nullptr}};
+    hipLaunchKernelGGL(k_norm_params, dim3((unsigned)((d.W + 15) / 16), 5, gate ? (unsigned)p.groups : 1u), dim3(256),
+                       0, st, p.part, p.gpart, wgs, p.groups, p.split, d.W, o);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace ga

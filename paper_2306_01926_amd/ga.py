@@ -22,12 +22,21 @@ SYMBOLS = ("ga_workspace_bytes", "ga_cluster", "ga_aggregate", "ga_attend", "ga_
            "ga_block_workspace_bytes", "ga_project_qkv", "ga_project_out", "ga_attention_block",
            "ga_merge_plan", "ga_next_group_count", "ga_backward_workspace_bytes", "ga_backward",
            "ga_timing_enable", "ga_timing_collect", "ga_status_string", "ga_last_error", "ga_workspace_check",
-           "ga_forward_noalloc")
+           "ga_forward_noalloc",
+           "ga_linear_workspace_bytes", "ga_linear_attend", "ga_linear_backward_workspace_bytes",
+           "ga_linear_backward", "ga_linear_step", "ga_rotary", "ga_norm_residual",
+           "ga_norm_backward_workspace_bytes", "ga_norm_residual_backward")
 
 
 class Shape(ctypes.Structure):
     _fields_ = [("B", ctypes.c_int32), ("H", ctypes.c_int32), ("n", ctypes.c_int32),
                 ("d", ctypes.c_int32), ("dtype", ctypes.c_int32)]
+
+
+class Norm(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("n", ctypes.c_int32), ("D", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("kind", ctypes.c_int32), ("gate_batches", ctypes.c_int32), ("eps", ctypes.c_float),
+                ("residual_scale", ctypes.c_float), ("branch_scale", ctypes.c_float)]
 
 
 class KernelTime(ctypes.Structure):
@@ -72,6 +81,22 @@ def lib() -> ctypes.CDLL:
         for f in ("ga_cluster", "ga_aggregate", "ga_attend", "ga_forward", "ga_forward_noalloc", "ga_project_qkv",
                   "ga_project_out",
                   "ga_attention_block", "ga_merge_plan", "ga_backward"):
+            getattr(L, f).restype = ctypes.c_int
+        f32, size = ctypes.c_float, ctypes.c_size_t
+        L.ga_linear_workspace_bytes.argtypes = [Shape, i32]
+        L.ga_linear_workspace_bytes.restype = size
+        L.ga_linear_attend.argtypes = [Shape, i32, P, P, P, P, P, P, f32, P, P, P, size, P]
+        L.ga_linear_backward_workspace_bytes.argtypes = [Shape, i32]
+        L.ga_linear_backward_workspace_bytes.restype = size
+        L.ga_linear_backward.argtypes = [Shape, i32, P, P, P, P, P, P, P, P, f32, P, P, P, P, P, size, P]
+        L.ga_linear_step.argtypes = [Shape, i32, P, P, P, P, P, i32, P, f32, P, P, P]
+        L.ga_rotary.argtypes = [Shape, i32, P, P, P, i32, i32, P, ctypes.c_double, i32, P, P, P]
+        L.ga_norm_residual.argtypes = [Norm, P, P, P, P, P, P, P, P, P, P]
+        L.ga_norm_backward_workspace_bytes.argtypes = [Norm]
+        L.ga_norm_backward_workspace_bytes.restype = size
+        L.ga_norm_residual_backward.argtypes = [Norm] + [P] * 17 + [size, P]
+        for f in ("ga_linear_attend", "ga_linear_backward", "ga_linear_step", "ga_rotary", "ga_norm_residual",
+                  "ga_norm_residual_backward"):
             getattr(L, f).restype = ctypes.c_int
         L.ga_workspace_check.argtypes = [Shape, i32, P, ctypes.c_size_t, P]
         L.ga_workspace_check.restype = ctypes.c_int
@@ -393,6 +418,215 @@ def backward(Q: torch.Tensor, dO: torch.Tensor, belong: torch.Tensor, centroid: 
     _check(lib().ga_backward(s, _p(Q), _p(dO), _p(belong), _p(centroid), _p(count), _p(vsum), int(N), scale, _p(dQ),
                              _p(dK), _p(dV), _p(ws), ws.numel(), _stream(dev)))
     return dQ, dK, dV
+
+
+def _launch(dev, call, *args) -> None:
+    """One entry point on the current stream of `dev`, with that device current."""
+    if dev.index is None or dev.index == torch.cuda.current_device():
+        _check(call(*args, _stream(dev)))
+        return
+    with torch.cuda.device(dev):
+        _check(call(*args, _stream(dev)))
+
+
+def _scratch(nbytes: int, dev, ws):
+    """(pointer, bytes) of a workspace: the caller's, or one of this call's own (so that captured graphs and
+    streams never share one).  The tensor is returned too, to live until the launch is enqueued."""
+    if ws is None:
+        if nbytes == 0:
+            return None, None, 0
+        ws = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+    else:
+        _expect(ws, "ws", dev, torch.uint8)
+    return ws, _p(ws), ws.numel()
+
+
+def _linear_args(Q, K, V, log_decay, lengths, state):
+    """Checks shared by the linear attention's calls; (shape, Hk, device, state shape)."""
+    dev = _qkv_like(Q, "Q")
+    s = shape_of(Q)
+    _expect(Q, "Q", dev, Q.dtype)
+    if not isinstance(K, torch.Tensor) or K.dim() != 4:
+        raise ValueError("K must be a [B, Hk, n, d] tensor")
+    B, H, n, d = Q.shape
+    Hk = K.shape[1]
+    _expect(K, "K", dev, Q.dtype, (B, Hk, n, d))
+    _expect(V, "V", dev, Q.dtype, (B, Hk, n, d))
+    _expect(log_decay, "log_decay", dev, torch.float32, (H,))
+    _expect(lengths, "lengths", dev, torch.int32, (B,), optional=True)
+    _expect(state, "state", dev, torch.float32, (B, H, d, d), optional=True)
+    return s, Hk, dev, (B, H, d, d)
+
+
+def linear_workspace_bytes(shape: Shape, Hk: int) -> int:
+    return int(lib().ga_linear_workspace_bytes(shape, int(Hk)))
+
+
+def linear_attend(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, log_decay: torch.Tensor,
+                  scale: float | None = None, lengths: torch.Tensor | None = None, state: torch.Tensor | None = None,
+                  return_state: bool = False, out: torch.Tensor | None = None, out_state: torch.Tensor | None = None,
+                  ws=None):
+    """Causal linear attention with a decay per head: O [B,H,n,64], or (O, state [B,H,64,64] fp32) if return_state.
+    K, V [B,Hk,n,64]; log_decay [H] fp32; lengths [B] int32; state: the state before the first token (out_state may
+    be that tensor itself)."""
+    s, Hk, dev, states = _linear_args(Q, K, V, log_decay, lengths, state)
+    _expect(out, "out", dev, Q.dtype, Q.shape, optional=True)
+    _expect(out_state, "out_state", dev, torch.float32, states, optional=True)
+    scale = 1.0 / math.sqrt(Q.shape[3]) if scale is None else float(scale)
+    O = torch.empty_like(Q) if out is None else out
+    if return_state and out_state is None:
+        out_state = torch.empty(states, dtype=torch.float32, device=dev)
+    ws, wp, nb = _scratch(lib().ga_linear_workspace_bytes(s, Hk), dev, ws)
+    _launch(dev, lib().ga_linear_attend, s, Hk, _p(Q), _p(K), _p(V), _p(log_decay), _p(lengths), _p(state), scale,
+            _p(O), _p(out_state), wp, nb)
+    return (O, out_state) if return_state else O
+
+
+def linear_backward_workspace_bytes(shape: Shape, Hk: int) -> int:
+    return int(lib().ga_linear_backward_workspace_bytes(shape, int(Hk)))
+
+
+def linear_backward(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, dO: torch.Tensor, log_decay: torch.Tensor,
+                    scale: float | None = None, lengths: torch.Tensor | None = None,
+                    state: torch.Tensor | None = None, dstate: torch.Tensor | None = None,
+                    return_dstate: bool = False, ws=None):
+    """Gradient of linear_attend: (dQ, dK, dV), and the initial state's gradient if return_dstate.  dstate: the
+    gradient that reaches the final state."""
+    s, Hk, dev, states = _linear_args(Q, K, V, log_decay, lengths, state)
+    _expect(dO, "dO", dev, Q.dtype, Q.shape)
+    _expect(dstate, "dstate", dev, torch.float32, states, optional=True)
+    scale = 1.0 / math.sqrt(Q.shape[3]) if scale is None else float(scale)
+    dQ, dK, dV = torch.empty_like(Q), torch.empty_like(K), torch.empty_like(V)
+    out = torch.empty(states, dtype=torch.float32, device=dev) if return_dstate else None
+    ws, wp, nb = _scratch(lib().ga_linear_backward_workspace_bytes(s, Hk), dev, ws)
+    _launch(dev, lib().ga_linear_backward, s, Hk, _p(Q), _p(K), _p(V), _p(dO), _p(log_decay), _p(lengths), _p(state),
+            _p(dstate), scale, _p(dQ), _p(dK), _p(dV), _p(out), wp, nb)
+    return (dQ, dK, dV, out) if return_dstate else (dQ, dK, dV)
+
+
+def linear_step(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, log_decay: torch.Tensor, state: torch.Tensor,
+                scale: float | None = None, slots: torch.Tensor | None = None, out: torch.Tensor | None = None,
+                out_state: torch.Tensor | None = None):
+    """One token per sequence (Q [B,H,1,64]) on kept states [states,H,64,64] fp32, updated in place unless out_state
+    is given: (O, the updated states).  slots [B] int32: the state of each batch row (outside the states: padding)."""
+    s, Hk, dev, _ = _linear_args(Q, K, V, log_decay, slots, None)
+    if not isinstance(state, torch.Tensor) or state.dim() != 4:
+        raise ValueError("state must be a [states, H, 64, 64] tensor")
+    _expect(state, "state", dev, torch.float32, (state.shape[0], Q.shape[1], Q.shape[3], Q.shape[3]))
+    _expect(out_state, "out_state", dev, torch.float32, state.shape, optional=True)
+    _expect(out, "out", dev, Q.dtype, Q.shape, optional=True)
+    scale = 1.0 / math.sqrt(Q.shape[3]) if scale is None else float(scale)
+    O = torch.empty_like(Q) if out is None else out
+    out_state = state if out_state is None else out_state
+    _launch(dev, lib().ga_linear_step, s, Hk, _p(Q), _p(K), _p(V), _p(log_decay), _p(slots), state.shape[0],
+            _p(state), scale, _p(O), _p(out_state))
+    return O, out_state
+
+
+ROTARY_INTERLEAVED, ROTARY_SHARED, ROTARY_INVERSE, ROTARY_FLOAT_POS = 1, 2, 4, 8
+
+
+def rotary(Q: torch.Tensor, K: torch.Tensor | None, pos: torch.Tensor, pairs, base: float = 10000.0,
+           interleaved: bool = False, shared: bool = False, inverse: bool = False, out=None):
+    """Rotary positions with several axes: (Q', K') for Q [B,H,n,64], K [B,Hk,n,64] (Q' alone if K is None).
+    pos [axes, B or 1, n] int32 or fp32; pairs: the feature pairs of each axis; shared: one ladder of frequencies over
+    all pairs instead of one per axis; inverse: the opposite turn, which is the gradient.  out: (Q', K') to write,
+    which may be Q and K themselves."""
+    dev = _qkv_like(Q, "Q")
+    s = shape_of(Q)
+    B, H, n, d = Q.shape
+    pairs = tuple(int(p) for p in pairs)
+    _expect(Q, "Q", dev, Q.dtype)
+    Hk = H
+    if K is not None:
+        if not isinstance(K, torch.Tensor) or K.dim() != 4:
+            raise ValueError("K must be a [B, Hk, n, d] tensor")
+        Hk = K.shape[1]
+        _expect(K, "K", dev, Q.dtype, (B, Hk, n, d))
+    if not isinstance(pos, torch.Tensor) or pos.dim() != 3 or pos.shape[1] not in (1, B):
+        raise ValueError(f"pos must be an [axes, 1 or {B}, n] tensor")
+    if pos.dtype not in (torch.int32, torch.float32):
+        raise ValueError(f"pos has dtype {pos.dtype}, expected int32 or float32")
+    _expect(pos, "pos", dev, pos.dtype, (len(pairs), pos.shape[1], n))
+    Qo, Ko = (torch.empty_like(Q), None if K is None else torch.empty_like(K)) if out is None else out
+    _expect(Qo, "out[0]", dev, Q.dtype, Q.shape)
+    if K is not None:
+        _expect(Ko, "out[1]", dev, Q.dtype, K.shape)
+    flags = (ROTARY_INTERLEAVED * bool(interleaved) + ROTARY_SHARED * bool(shared) + ROTARY_INVERSE * bool(inverse)
+             + ROTARY_FLOAT_POS * (pos.dtype == torch.float32))
+    _launch(dev, lib().ga_rotary, s, Hk, _p(Q), _p(K), _p(pos), pos.shape[1], len(pairs),
+            (ctypes.c_int32 * len(pairs))(*pairs), float(base), flags, _p(Qo), _p(Ko))
+    return Qo if K is None else (Qo, Ko)
+
+
+NORMS = {"rms": 0, "layer": 1}
+
+
+def _norm_args(X, F, norm, eps, post_weight, post_bias, gate, pre_weight, pre_bias, residual_scale, branch_scale):
+    """Checks shared by the norm's calls; (ga_norm_t, device, the tensors' pointers)."""
+    if not isinstance(X, torch.Tensor) or X.dim() != 3:
+        raise ValueError("X must be a [B, n, D] tensor")
+    if norm not in NORMS:
+        raise ValueError(f"norm must be one of {sorted(NORMS)} (got {norm!r})")
+    dev = _device_of(X)
+    B, n, D = X.shape
+    code = _dtype_code(X)
+    _expect(X, "X", dev, X.dtype)
+    _expect(F, "F", dev, X.dtype, X.shape, optional=True)
+    for t, name in ((post_weight, "post_weight"), (post_bias, "post_bias"), (pre_weight, "pre_weight"),
+                    (pre_bias, "pre_bias")):
+        _expect(t, name, dev, X.dtype, (D,), optional=True)
+    batches = 0
+    if gate is not None:
+        if not isinstance(gate, torch.Tensor) or gate.dim() not in (1, 2):
+            raise ValueError("gate must be a [D] or [B, D] tensor")
+        batches = 1 if gate.dim() == 1 else B
+        _expect(gate, "gate", dev, X.dtype, (D,) if gate.dim() == 1 else (B, D))
+    s = Norm(B, n, D, code, NORMS[norm], batches, eps, residual_scale, branch_scale)
+    return s, dev, [_p(t) for t in (X, F, post_weight, post_bias, gate, pre_weight, pre_bias)]
+
+
+def norm_residual(X: torch.Tensor, F: torch.Tensor | None = None, norm: str = "rms", eps: float = 1e-6,
+                  post_weight=None, post_bias=None, gate=None, pre_weight=None, pre_bias=None,
+                  residual_scale: float = 1.0, branch_scale: float = 1.0, return_sum: bool = True):
+    """Y = residual_scale X + branch_scale gate * post_norm(F) and, with pre_weight, H = pre_norm(Y): returns Y,
+    (Y, H), or H alone without return_sum.  X, F [B,n,D]; weights and biases [D]; gate [D] or [B,D]; norm "rms" or
+    "layer"; no post_weight: F itself; no F: the residual stream alone."""
+    s, dev, tensors = _norm_args(X, F, norm, eps, post_weight, post_bias, gate, pre_weight, pre_bias, residual_scale,
+                                 branch_scale)
+    Y = torch.empty_like(X) if return_sum else None
+    H = torch.empty_like(X) if pre_weight is not None else None
+    _launch(dev, lib().ga_norm_residual, s, *tensors, _p(Y), _p(H))
+    return H if Y is None else Y if H is None else (Y, H)
+
+
+def norm_backward_workspace_bytes(s: Norm) -> int:
+    return int(lib().ga_norm_backward_workspace_bytes(s))
+
+
+def norm_residual_backward(X: torch.Tensor, F: torch.Tensor | None, dY: torch.Tensor | None,
+                           dH: torch.Tensor | None = None, norm: str = "rms", eps: float = 1e-6, post_weight=None,
+                           post_bias=None, gate=None, pre_weight=None, pre_bias=None, residual_scale: float = 1.0,
+                           branch_scale: float = 1.0, ws=None) -> dict:
+    """Gradient of norm_residual from those of Y and H (each may be None): a dict of dX, dF (X's dtype) and, for what
+    the call has, dpost_w, dpost_b, dgate, dpre_w, dpre_b (fp32 sums over the tokens)."""
+    s, dev, tensors = _norm_args(X, F, norm, eps, post_weight, post_bias, gate, pre_weight, pre_bias, residual_scale,
+                                 branch_scale)
+    _expect(dY, "dY", dev, X.dtype, X.shape, optional=True)
+    _expect(dH, "dH", dev, X.dtype, X.shape, optional=True)
+    B, _, D = X.shape
+    empty = torch.empty if B else torch.zeros  # no tokens: nothing is enqueued, every sum is zero
+
+    def sums(wanted, *shape):
+        return empty(shape, dtype=torch.float32, device=dev) if wanted else None
+
+    got = dict(dX=torch.empty_like(X), dF=None if F is None else torch.empty_like(F),
+               dpost_w=sums(post_weight is not None, D), dpost_b=sums(post_bias is not None, D),
+               dgate=None if gate is None else sums(True, *gate.shape),
+               dpre_w=sums(dH is not None, D), dpre_b=sums(dH is not None and pre_bias is not None, D))
+    ws, wp, nb = _scratch(lib().ga_norm_backward_workspace_bytes(s), dev, ws)
+    _launch(dev, lib().ga_norm_residual_backward, s, *tensors, _p(dY), _p(dH), *(_p(t) for t in got.values()), wp, nb)
+    return {k: t for k, t in got.items() if t is not None}
 
 
 def workspace_check(X: torch.Tensor, N: int, ws=None) -> None:
