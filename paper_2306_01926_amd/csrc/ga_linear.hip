@@ -15,6 +15,9 @@
 
 #include <float.h>
 #include <stdint.h>
+#include <stdlib.h>
+
+#include <type_traits>
 
 #include "ga_internal.h"
 
@@ -208,17 +211,17 @@ __global__ __launch_bounds__(256) void k_lin_heads(const float* __restrict__ par
 // A chunk of 64 tokens is computed from the state before it:
 //   O = scale ((Q K^T * D) V + diag(l^{i+1}) Q S),  D_ij = l^{i-j} for j <= i,
 //   S' = l^64 S + sum_j l^{63-j} k_j v_j^T,
-// all four products on the matrix cores.  A workgroup of four waves walks the
-// chunks of one slice, or of one of P segments of it; wave (rb, ch) owns the
-// 32 tokens rb and the 32 value features ch of the output, and the quadrant
-// (features 32 rb of k) x (features 32 ch of v) of the state in 16 registers.
+// all four products on the matrix cores.  A workgroup of eight waves walks the
+// chunks of one slice, or of one of P segments of it: four waves form the
+// output, 32 tokens by 32 value features each, four the state, a quadrant each
+// in 16 registers, one chunk ahead of its use.
 //
 // Products are formed transposed (K Q^T, V^T P^T, ...), so the scores' result
 // registers are the next product's operand as they are: no LDS round trip.
 // The value rows feeding the last product are permuted so that a lane ends with
 // 16 consecutive features of one token (32 bytes, stored from registers).
-// K and V rows sit in LDS as they come (16-byte granules XOR-swizzled by row);
-// the operands that need a column of them come from transposing LDS reads.
+// K and V rows sit in LDS as they come; the operands that need a column of them
+// come from transposing LDS reads.  Q goes to registers directly.
 //
 // Roundings: the scores after decay and the state that Q meets are rounded to
 // bf16, as the matrix cores need (each term of an output passes one of the
@@ -252,246 +255,430 @@ __device__ __forceinline__ f32x16 zero16() {
   return z;
 }
 
-// Byte offset of 16-byte granule q of row r of a tile: the key takes all eight
-// values on eight consecutive rows, so that reads of one granule of many rows
-// and transposing reads of four rows spread over the banks.
-__device__ __forceinline__ int tkey(int r) { return (r & 7) ^ ((r >> 3) & 1); }
-__device__ __forceinline__ int toff(int r, int q) { return r * 128 + ((q ^ tkey(r)) << 4); }
+// Byte offset of 16-byte granule q of row r of a tile of 128-byte rows.  The
+// granule is XORed with a key of the row: rows two apart differ in its highest
+// bit, so a transposing read's four rows of 64 bytes meet all 64 banks once,
+// and eight rows of equal parity in all of it, as do 16 rows of one granule.
+__device__ __forceinline__ int toff(int r, int q) {
+  const int m = r >> 1;
+  return r * 128 + ((q ^ (((m & 1) << 2) | (m & 2) | ((m >> 2) & 1))) << 4);
+}
+// A buffer of `bytes` bytes at p for loads and stores whose lanes beyond it read
+// zeros and write nothing.  The walks below load and store without branches, so
+// that the compiler can count what is in flight and wait for the oldest alone.
+typedef __amdgpu_buffer_rsrc_t Buffer;
+__device__ __forceinline__ Buffer buffer(const void* p, int bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc((void*)p, 0, bytes, 0x00027000);
+}
+__device__ __forceinline__ u32x4 buf_load(Buffer b, int off) {
+  return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(b, off, 0, 0));
+}
+__device__ __forceinline__ void buf_store(Buffer b, int off, u32x4 x) {
+  __builtin_amdgcn_raw_buffer_store_b128(x, b, off, 0, 0);
+}
 
 struct Chunked {
   const uint16_t *q, *k, *v;          // roles (see the head of the file)
   bool q_shared, k_shared, v_shared;  // the tensor has Hk heads
   const float *log_decay, *state;
   const int32_t* lengths;
-  float* seg;        // [B H][P][64][64]: local states (STATES), then the states before each segment; P > 1 only
+  float* seg;        // [B H][P][64][64]: the segments' local states, or (scanned) the states before them; P > 1 only
   float* state_out;
   void* out;
   int H, Hk, n, P, cps;  // segments per slice, chunks per segment
   float scale;
-  bool transposed, out_f32;
+  bool transposed, scanned;
 };
 
+// One segment of one slice, as its workgroup sees it.
 // REV walks from a sequence's last token to its first; its state is R of the
 // head of the file times l, the carry to the token before: a token's own decay
 // is behind it, so the exponents are one lower at the output and one higher in
 // the sum, and the scale sits in the sum.
-// STATES: the local states of the segments alone (from zero; no output).
-template <bool REV, bool STATES>
-__global__ __launch_bounds__(256, 2) void k_lin_chunk(Chunked A) {
-  constexpr int kTiles = STATES ? 3 : 4;  // V, K hi, K lo (decayed), K
-  __shared__ __attribute__((aligned(16))) unsigned char lds[2 * kTiles * kTile + (STATES ? 0 : 2 * kTile)];
-  const int nseg = STATES ? A.P - 1 : A.P;
-  const int64_t bh = blockIdx.x / nseg;
-  const int p = (int)(blockIdx.x - bh * nseg);
-  const int h = (int)(bh % A.H);
-  const int64_t b = bh / A.H, bk = b * A.Hk + h / (A.H / A.Hk);
-  const int len = length_of(A.lengths, b, A.n);
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int rb = wave & 1, ch = wave >> 1, r = lane & 31, hf = lane >> 5;
-  const uint16_t* q = A.q + (A.q_shared ? bk : bh) * A.n * 64;
-  const uint16_t* k = A.k + (A.k_shared ? bk : bh) * A.n * 64;
-  const uint16_t* v = A.v + (A.v_shared ? bk : bh) * A.n * 64;
-  const float g = decay_log2(A.log_decay[h]);
-  const int c0 = p * A.cps, c1 = min(c0 + A.cps, (len + kC - 1) / kC);
-  auto row = [&](int t) __attribute__((always_inline)) {  // first feature of walk position t (clamped)
-    const int x = min(t, len - 1);
-    return (int64_t)(REV ? len - 1 - x : x) * 64;
-  };
+template <bool REV>
+struct Segment {
+  const uint16_t *q, *k, *v;
+  int64_t bh;
+  int p, len, c0, c1;
+  float g, ks;
 
-  // the state's quadrant: S[a][c], a = 32 rb + r, c = 32 ch + 16 hf + 0..15
-  const int sa = 32 * rb + r, sc = 32 * ch + 16 * hf;
-  f32x16 S = zero16();
-  if (!STATES) {
-    const float* s0 = A.P > 1 ? A.seg + (bh * A.P + p) * 4096 : (A.state ? A.state + bh * 4096 : nullptr);
-    if (s0 && (A.P > 1 || !A.transposed)) {
+  __device__ __forceinline__ Segment(const Chunked& A, int64_t slice, int segment) : bh(slice), p(segment) {
+    const int h = (int)(bh % A.H);
+    const int64_t b = bh / A.H, bk = b * A.Hk + h / (A.H / A.Hk);
+    len = __builtin_amdgcn_readfirstlane(length_of(A.lengths, b, A.n));
+    q = A.q + (A.q_shared ? bk : bh) * A.n * 64;
+    k = A.k + (A.k_shared ? bk : bh) * A.n * 64;
+    v = A.v + (A.v_shared ? bk : bh) * A.n * 64;
+    g = decay_log2(A.log_decay[h]);
+    ks = REV ? A.scale : 1.f;
+    c0 = p * A.cps;
+    c1 = min(c0 + A.cps, (len + kC - 1) / kC);
+  }
+  // rows of chunk c (none behind the segment), the first one in memory, and
+  // the place of walk row x among them (beyond them: out of the buffer)
+  __device__ __forceinline__ int count(int c) const { return c < c1 ? min(len - c * kC, kC) : 0; }
+  __device__ __forceinline__ int64_t first(int c, int nr) const {
+    return REV ? (int64_t)len - (int64_t)c * kC - nr : (int64_t)c * kC;
+  }
+  __device__ __forceinline__ int place(int x, int nr) const { return REV ? nr - 1 - x : x; }
+  // tokens of segment u
+  __device__ __forceinline__ float tokens(const Chunked& A, int u) const {
+    const int64_t t = (int64_t)A.cps * kC;
+    return (float)min(max((int64_t)len - u * t, (int64_t)0), t);
+  }
+  // granule x of row rr of chunk c, decayed to the chunk's end, in two bf16 parts
+  __device__ __forceinline__ void decayed(u32x4 x, int rr, int c, u32x4& hi, u32x4& lo) const {
+    // rows behind the end are zeros
+    const float w = ks * decay_pow(g, (float)(max(count(c) - 1 - rr, 0) + REV));
 #pragma unroll
-      for (int x = 0; x < 16; x += 4) {
-        const float4 f = *(const float4*)(s0 + sa * 64 + sc + x);
-        S[x] = f.x, S[x + 1] = f.y, S[x + 2] = f.z, S[x + 3] = f.w;
-      }
-    } else if (s0) {
-#pragma unroll
-      for (int x = 0; x < 16; ++x) S[x] = s0[(sc + x) * 64 + sa];
+    for (int e = 0; e < 4; ++e) {
+      const float a = w * bf16_to_f32(x[e] & 0xffffu), b = w * __uint_as_float(x[e] & 0xffff0000u);
+      hi[e] = pack_bf16x2(a, b);
+      lo[e] = pack_bf16x2(a - bf16_to_f32(hi[e] & 0xffffu), b - __uint_as_float(hi[e] & 0xffff0000u));
     }
   }
-  unsigned char* stile = lds + 2 * kTiles * kTile;
-  auto put_state = [&](int buf) __attribute__((always_inline)) {
-    u32x4 lo, hi;
-#pragma unroll
-    for (int x = 0; x < 4; ++x) {
-      lo[x] = pack_bf16x2(S[2 * x], S[2 * x + 1]);
-      hi[x] = pack_bf16x2(S[8 + 2 * x], S[9 + 2 * x]);
-    }
-    *(u32x4*)(stile + buf * kTile + toff(sa, sc / 8)) = lo;
-    *(u32x4*)(stile + buf * kTile + toff(sa, sc / 8 + 1)) = hi;
-  };
-
-  // staging: thread tid moves granule tid % 8 of rows tid / 8 and 32 + tid / 8
-  const int gr = tid & 7, r0 = tid >> 3;
-  u32x4 gk[2], gv[2], qf[4], qn[4];
-  auto load = [&](int c) __attribute__((always_inline)) {
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const int64_t at = row(c * kC + r0 + 32 * u) + 8 * gr;
-      gk[u] = *(const u32x4*)(k + at);
-      gv[u] = *(const u32x4*)(v + at);
-    }
-    if (!STATES) {
-      const uint16_t* qr = q + row(c * kC + 32 * rb + r) + 8 * hf;
-#pragma unroll
-      for (int s = 0; s < 4; ++s) qn[s] = *(const u32x4*)(qr + 16 * s);
-    }
-  };
-  const float ks = REV ? A.scale : 1.f;
-  float wk[2];
-#pragma unroll
-  for (int u = 0; u < 2; ++u) wk[u] = ks * decay_pow(g, (float)(kC - 1 + REV - (r0 + 32 * u)));
-  auto stage = [&](int c, int buf) __attribute__((always_inline)) {
-    unsigned char* t = lds + buf * kTiles * kTile;
-    const int rem = len - c * kC;  // rows of this chunk
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const int rr = r0 + 32 * u, at = toff(rr, gr);
-      float w = wk[u];
-      if (rem < kC) {
-        w = rr < rem ? ks * decay_pow(g, (float)(rem - 1 + REV - rr)) : 0.f;
-        if (rr >= rem) gk[u] = gv[u] = u32x4{0u, 0u, 0u, 0u};
-      }
-      u32x4 hi, lo;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float x = w * bf16_to_f32(gk[u][e] & 0xffffu), y = w * __uint_as_float(gk[u][e] & 0xffff0000u);
-        hi[e] = pack_bf16x2(x, y);
-        lo[e] = pack_bf16x2(x - bf16_to_f32(hi[e] & 0xffffu), y - __uint_as_float(hi[e] & 0xffff0000u));
-      }
-      *(u32x4*)(t + at) = gv[u];
-      *(u32x4*)(t + kTile + at) = hi;
-      *(u32x4*)(t + 2 * kTile + at) = lo;
-      if (!STATES) *(u32x4*)(t + 3 * kTile + at) = gk[u];
-    }
-  };
-
-  // transposing reads: lane 4 j + s of a block of 16 addresses row j
-  const int bj = (lane >> 2) & 3, bs = lane & 3, bb = (lane >> 4) & 1;
-  // columns 32 ch ..: permuted so that result row 8 (v / 4) + 4 hf + v % 4 is column 16 hf + v
-  auto tr_perm = [&](const unsigned char* t, int rw) __attribute__((always_inline)) {
-    return lds_tr16(t + toff(rw + bj, 4 * ch + 2 * (bs & 1) + bb) + 8 * (bs >> 1));
-  };
-  // columns 32 rb .. in order
-  auto tr_nat = [&](const unsigned char* t, int rw) __attribute__((always_inline)) {
-    return lds_tr16(t + toff(rw + bj, 4 * rb + 2 * bb + (bs >> 1)) + 8 * (bs & 1));
-  };
-
-  float wd[16], wo[16];
-#pragma unroll
-  for (int x = 0; x < 16; ++x) {
-    const int d = r - (8 * (x / 4) + 4 * hf + x % 4);  // query minus key within a block
-    wd[x] = d >= 0 ? A.scale * decay_pow(g, (float)d) : 0.f;
-    wo[x] = A.scale * decay_pow(g, (float)(32 + d));
-  }
-  const float wi = (REV ? 1.f : A.scale) * decay_pow(g, (float)(32 * rb + r + 1 - REV));
-  const float wc = decay_pow(g, (float)kC);
-
-  if (c0 < c1) {
-    load(c0);
-    stage(c0, 0);
-    if (!STATES) {
-      put_state(0);
-#pragma unroll
-      for (int s = 0; s < 4; ++s) qf[s] = qn[s];
-    }
+  // Walks the segment's chunks: load(c, R) requests the rows of chunk c, three
+  // chunks ahead of their use (HBM answers after about the time of two),
+  // put(c, buf, R) puts them into a tile buffer, step(c, buf, R) computes chunk
+  // c and puts the next chunk's rows R into the other buffer: one barrier a
+  // chunk.  Three chunks a turn, as many sets of registers, and no way out
+  // between them, which would cost copies of rows in flight (a wait for them).
+  template <class Rows, class Load, class Put, class Step>
+  __device__ __forceinline__ void walk(Load load, Put put, Step step) const {
+    if (c0 >= c1) return;
+    Rows R0, R1, R2;
+    load(c0, R0);
+    load(c0 + 1, R1);
+    load(c0 + 2, R2);
+    put(c0, 0, R0);
     __syncthreads();
+    auto turn = [&](int c, int buf, const Rows& next, Rows& later) __attribute__((always_inline)) {
+      load(c + 3, later);
+      step(c, buf, next);
+      __syncthreads();
+    };
+    int c = c0, buf = 0;
+    for (; c + 3 <= c1; c += 3, buf ^= 1) {
+      turn(c, buf, R1, R0);
+      turn(c + 1, buf ^ 1, R2, R1);
+      turn(c + 2, buf, R0, R2);
+    }
+    if (c < c1) turn(c, buf, R1, R0);
+    if (c + 1 < c1) turn(c + 1, buf ^ 1, R2, R1);
   }
-  for (int c = c0; c < c1; ++c) {
-    const int buf = (c - c0) & 1;
-    const unsigned char* t = lds + buf * kTiles * kTile;
-    const bool more = c + 1 < c1;
-    if (more) load(c + 1);
-    u32x4 vf[4];  // V^T: step x contracts tokens 16 x + {4 hf + 0..3, 8 + 4 hf + 0..3}
+};
+
+// Lane numbers of the operands: the transposing reads' row and 8-byte piece.
+struct Lanes {
+  int r, hf, bj, bs, bb;
+  __device__ __forceinline__ explicit Lanes(int lane)
+      : r(lane & 31), hf(lane >> 5), bj((lane >> 2) & 3), bs(lane & 3), bb((lane >> 4) & 1) {}
+  // four rows from rw: columns 32 half .. in order, of a tile of 128-byte rows
+  __device__ __forceinline__ u32x2 nat(const unsigned char* t, int rw, int half) const {
+    return lds_tr16(t + toff(rw + bj, 4 * half + 2 * bb + (bs >> 1)) + 8 * (bs & 1));
+  }
+  // columns 32 half .. permuted so that result row 8 (v / 4) + 4 hf + v % 4 is column 16 hf + v
+  __device__ __forceinline__ u32x2 perm(const unsigned char* t, int rw, int half) const {
+    return lds_tr16(t + toff(rw + bj, 4 * half + 2 * (bs & 1) + bb) + 8 * (bs >> 1));
+  }
+};
+
+// The local states of the segments but the last, from zero: four waves, a
+// quadrant of the state each.  grid: slices (P - 1).
+template <bool REV>
+__global__ __launch_bounds__(256, 3) void k_lin_states(Chunked A) {
+  __shared__ __attribute__((aligned(16))) unsigned char lds[2][3 * kTile];  // V, K hi, K lo (decayed)
+  const int64_t bh = blockIdx.x / (A.P - 1);
+  const Segment<REV> G(A, bh, (int)(blockIdx.x - bh * (A.P - 1)));
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const Lanes L(tid & 63);
+  const int ah = wave & 1, ch = wave >> 1, gr = tid & 7, r0 = tid >> 3;
+  struct Rows {
+    u32x4 k[2], v[2];
+  };
+  f32x16 S = zero16();
+  auto put = [&](int c, int buf, const Rows& R) __attribute__((always_inline)) {
 #pragma unroll
-    for (int x = 0; x < 4; ++x) vf[x] = join(tr_perm(t, 16 * x + 4 * hf), tr_perm(t, 16 * x + 8 + 4 * hf));
-    if (!STATES) {
-      u32x4 pf[4];
+    for (int u = 0; u < 2; ++u) {
+      u32x4 hi, lo;
+      G.decayed(R.k[u], r0 + 32 * u, c, hi, lo);
+      const int at = toff(r0 + 32 * u, gr);
+      *(u32x4*)(lds[buf] + at) = R.v[u];
+      *(u32x4*)(lds[buf] + kTile + at) = hi;
+      *(u32x4*)(lds[buf] + 2 * kTile + at) = lo;
+    }
+  };
+  G.template walk<Rows>(
+      [&](int c, Rows& R) __attribute__((always_inline)) {
+        const int nr = G.count(c);
+        const Buffer bk = buffer(G.k + G.first(c, nr) * 64, nr * 128), bv = buffer(G.v + G.first(c, nr) * 64, nr * 128);
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb) {
-        if (kb > rb) continue;
-        f32x16 P = zero16();
+        for (int u = 0; u < 2; ++u) {
+          const int off = G.place(r0 + 32 * u, nr) * 128 + 16 * gr;
+          R.k[u] = buf_load(bk, off);
+          R.v[u] = buf_load(bv, off);
+        }
+      },
+      put,
+      [&](int c, int buf, const Rows& next) __attribute__((always_inline)) {
+        const unsigned char* t = lds[buf];
+        const float w = decay_pow(G.g, (float)G.count(c));
+        u32x4 vf[4], kh[4], kl[4];  // step x contracts tokens 16 x + {4 hf + 0..3, 8 + 4 hf + 0..3}
 #pragma unroll
-        for (int s = 0; s < 4; ++s)
-          P = mfma(*(const u32x4*)(t + 3 * kTile + toff(32 * kb + r, 2 * s + hf)), qf[s], P);
+        for (int x = 0; x < 4; ++x) {
+          const int ra = 16 * x + 4 * L.hf;
+          vf[x] = join(L.perm(t, ra, ch), L.perm(t, ra + 8, ch));
+          kh[x] = join(L.nat(t + kTile, ra, ah), L.nat(t + kTile, ra + 8, ah));
+          kl[x] = join(L.nat(t + 2 * kTile, ra, ah), L.nat(t + 2 * kTile, ra + 8, ah));
+        }
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
+        for (int x = 0; x < 16; ++x) S[x] *= w;
+        f32x16 T = zero16();
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int x = 8 * u + 2 * e;
-            pf[2 * kb + u][e] = kb == rb ? pack_bf16x2(P[x] * wd[x], P[x + 1] * wd[x + 1])
-                                         : pack_bf16x2(P[x] * wo[x], P[x + 1] * wo[x + 1]);
-          }
+        for (int x = 0; x < 4; ++x) {
+          S = mfma(vf[x], kh[x], S);
+          T = mfma(vf[x], kl[x], T);
+        }
+        put(c + 1, buf ^ 1, next);
+#pragma unroll
+        for (int x = 0; x < 16; ++x) S[x] += T[x];
+      });
+  float* so = A.seg + (bh * A.P + G.p) * 4096 + (32 * ah + L.r) * 64 + 32 * ch + 16 * L.hf;
+#pragma unroll
+  for (int x = 0; x < 16; x += 4) *(float4*)(so + x) = make_float4(S[x], S[x + 1], S[x + 2], S[x + 3]);
+}
+
+// Outputs (and the final state).  OUT32: the output is fp32 (a query head's
+// share of a shared head's gradient).  grid: slices P.
+template <bool REV, bool OUT32>
+__global__ __launch_bounds__(512, 2) void k_lin_chunk(Chunked A) {
+  constexpr int kBuf = 6 * kTile;  // K, K hi, K lo (decayed), V, the state, Q
+  __shared__ __attribute__((aligned(16))) unsigned char lds[2][kBuf];
+  const int64_t bh = blockIdx.x / A.P;
+  const Segment<REV> G(A, bh, (int)(blockIdx.x - bh * A.P));
+  // the wave's index is scalar, so that branches on it are jumps: matrix
+  // instructions do not heed the lane mask
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lane = tid & 63;
+  const Lanes L(lane);
+  constexpr int kV = 3 * kTile, kS = 4 * kTile, kQ = 5 * kTile;
+  const int ch = (wave >> 1) & 1;
+
+  if (wave >= 4) {
+    // the state S[a][c], a = 32 ah + r, c = 32 ch + 16 hf + 0..15; its waves
+    // also bring the keys: granule tid % 8 of two rows 32 apart
+    const int ah = wave & 1, sa = 32 * ah + L.r, sc = 32 * ch + 16 * L.hf, gr = tid & 7, r0 = (tid >> 3) & 31;
+    struct Rows {
+      u32x4 k[2];
+    };
+    f32x16 S = zero16();
+    const bool given = A.state && !A.scanned;
+    if (A.scanned || (given && !A.transposed)) {
+      const float* s0 = (A.scanned ? A.seg + (bh * A.P + G.p) * 4096 : A.state + bh * 4096) + sa * 64 + sc;
+#pragma unroll
+      for (int x = 0; x < 16; ++x) S[x] = s0[x];
+    } else if (given) {
+#pragma unroll
+      for (int x = 0; x < 16; ++x) S[x] = A.state[bh * 4096 + (sc + x) * 64 + sa];
+    }
+    if (!A.scanned) {
+      for (int u = 0; u < G.p; ++u) {
+        const float w = decay_pow(G.g, G.tokens(A, u));
+        const float* s0 = A.seg + (bh * A.P + u) * 4096 + sa * 64 + sc;
+#pragma unroll
+        for (int x = 0; x < 16; ++x) S[x] = fmaf(w, S[x], s0[x]);
       }
-      f32x16 o = zero16();
-      const unsigned char* st = stile + buf * kTile;
+    }
+    u32x4 hi[2], lo[2];
+    auto convert = [&](int c, const Rows& R) __attribute__((always_inline)) {
 #pragma unroll
-      for (int s = 0; s < 4; ++s)
-        o = mfma(join(tr_perm(st, 16 * s + 8 * hf), tr_perm(st, 16 * s + 8 * hf + 4)), qf[s], o);
+      for (int u = 0; u < 2; ++u) G.decayed(R.k[u], r0 + 32 * u, c, hi[u], lo[u]);
+    };
+    auto put = [&](int buf, const Rows& R) __attribute__((always_inline)) {
 #pragma unroll
-      for (int x = 0; x < 16; ++x) o[x] *= wi;
+      for (int u = 0; u < 2; ++u) {
+        const int at = toff(r0 + 32 * u, gr);
+        *(u32x4*)(lds[buf] + at) = R.k[u];
+        *(u32x4*)(lds[buf] + kTile + at) = hi[u];
+        *(u32x4*)(lds[buf] + 2 * kTile + at) = lo[u];
+      }
+    };
+    auto put_state = [&](int buf) __attribute__((always_inline)) {
 #pragma unroll
-      for (int x = 0; x < 4; ++x)
-        if (x / 2 <= rb) o = mfma(vf[x], pf[x], o);
-      const int i = c * kC + 32 * rb + r;
-      if (i < len) {
-        const int64_t at = bh * A.n * 64 + row(i) + sc;
-        if (A.out_f32) {
+      for (int x = 0; x < 16; x += 8)
+        *(u32x4*)(lds[buf] + kS + toff(sa, 4 * ch + 2 * L.hf + x / 8)) =
+            u32x4{pack_bf16x2(S[x], S[x + 1]), pack_bf16x2(S[x + 2], S[x + 3]), pack_bf16x2(S[x + 4], S[x + 5]),
+                  pack_bf16x2(S[x + 6], S[x + 7])};
+    };
+    G.template walk<Rows>(
+        [&](int c, Rows& R) __attribute__((always_inline)) {
+          const int nr = G.count(c);
+          const Buffer bk = buffer(G.k + G.first(c, nr) * 64, nr * 128);
 #pragma unroll
-          for (int x = 0; x < 16; x += 4)
-            *(float4*)((float*)A.out + at + x) = make_float4(o[x], o[x + 1], o[x + 2], o[x + 3]);
-        } else {
-          u32x4 lo, hi;
+          for (int u = 0; u < 2; ++u) R.k[u] = buf_load(bk, G.place(r0 + 32 * u, nr) * 128 + 16 * gr);
+        },
+        [&](int c, int buf, const Rows& R) __attribute__((always_inline)) {
+          convert(c, R);
+          put(buf, R);
+          put_state(buf);
+        },
+        [&](int c, int buf, const Rows& next) __attribute__((always_inline)) {
+          const unsigned char* t = lds[buf];
+          const float w = decay_pow(G.g, (float)G.count(c));
+          // the conversion comes first: the output's waves have the LDS then
+          convert(c + 1, next);
+#pragma unroll
+          for (int x = 0; x < 16; ++x) S[x] *= w;
+          __builtin_amdgcn_sched_barrier(0);
+          u32x4 vf[4], kh[4], kl[4];  // step x contracts tokens 16 x + {4 hf + 0..3, 8 + 4 hf + 0..3}
 #pragma unroll
           for (int x = 0; x < 4; ++x) {
-            lo[x] = pack_bf16x2(o[2 * x], o[2 * x + 1]);
-            hi[x] = pack_bf16x2(o[8 + 2 * x], o[9 + 2 * x]);
+            const int ra = 16 * x + 4 * L.hf;
+            vf[x] = join(L.perm(t + kV, ra, ch), L.perm(t + kV, ra + 8, ch));
+            kh[x] = join(L.nat(t + kTile, ra, ah), L.nat(t + kTile, ra + 8, ah));
+            kl[x] = join(L.nat(t + 2 * kTile, ra, ah), L.nat(t + 2 * kTile, ra + 8, ah));
           }
-          *(u32x4*)((uint16_t*)A.out + at) = lo;
-          *(u32x4*)((uint16_t*)A.out + at + 8) = hi;
+          f32x16 T = zero16();
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            S = mfma(vf[x], kh[x], S);
+            T = mfma(vf[x], kl[x], T);
+          }
+          __builtin_amdgcn_sched_group_barrier(0x100, 12, 0);
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            __builtin_amdgcn_sched_group_barrier(0x8, 2, 0);
+            if (x < 2) __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
+          }
+          __builtin_amdgcn_sched_barrier(0);
+          put(buf ^ 1, next);
+#pragma unroll
+          for (int x = 0; x < 16; ++x) S[x] += T[x];
+          put_state(buf ^ 1);
+        });
+    if (G.p == A.P - 1 && A.state_out) {
+      float* so = A.state_out + bh * 4096 + sa * 64 + sc;
+#pragma unroll
+      for (int x = 0; x < 16; x += 4) *(float4*)(so + x) = make_float4(S[x], S[x + 1], S[x + 2], S[x + 3]);
+    }
+  } else {
+    float wd[16], wo[16];  // decays inside a block of 32 tokens, and between two
+#pragma unroll
+    for (int x = 0; x < 16; ++x) {
+      const int d = L.r - (8 * (x / 4) + 4 * L.hf + x % 4);  // query minus key within a block
+      wd[x] = d >= 0 ? A.scale * decay_pow(G.g, (float)d) : 0.f;
+      wo[x] = A.scale * decay_pow(G.g, (float)(32 + d));
+    }
+    constexpr int kEl = OUT32 ? 4 : 2;
+    unsigned char* out = (unsigned char*)A.out + bh * A.n * (64 * kEl);
+    // the values and queries: granule tid % 8 of rows tid / 8 and 32 + tid / 8
+    const int gr = tid & 7, r0 = tid >> 3;
+    struct Rows {
+      u32x4 v[2], q[2];
+    };
+    // the second block of tokens meets two blocks of keys, the first one: a
+    // loop for each, without branches
+    auto outputs = [&](auto block) __attribute__((always_inline)) {
+      constexpr int RB = decltype(block)::value;
+      const float wi = (REV ? 1.f : A.scale) * decay_pow(G.g, (float)(32 * RB + L.r + 1 - REV));
+      auto put = [&](int, int buf, const Rows& R) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          *(u32x4*)(lds[buf] + kV + toff(r0 + 32 * u, gr)) = R.v[u];
+          *(u32x4*)(lds[buf] + kQ + toff(r0 + 32 * u, gr)) = R.q[u];
         }
-      }
-    }
-    const float w = len - c * kC < kC ? decay_pow(g, (float)(len - c * kC)) : wc;
+      };
+      G.template walk<Rows>(
+          [&](int c, Rows& R) __attribute__((always_inline)) {
+            const int nr = G.count(c);
+            const Buffer bv = buffer(G.v + G.first(c, nr) * 64, nr * 128), bq = buffer(G.q + G.first(c, nr) * 64, nr * 128);
 #pragma unroll
-    for (int x = 0; x < 16; ++x) S[x] *= w;
+            for (int u = 0; u < 2; ++u) {
+              const int off = G.place(r0 + 32 * u, nr) * 128 + 16 * gr;
+              R.v[u] = buf_load(bv, off);
+              R.q[u] = buf_load(bq, off);
+            }
+          },
+          put,
+          [&](int c, int buf, const Rows& next) __attribute__((always_inline)) {
+            const unsigned char* t = lds[buf];
+            u32x4 qf[4], kf[RB + 1][4], sf[4], vf[2 * RB + 2], pf[2 * RB + 2];
 #pragma unroll
-    for (int x = 0; x < 4; ++x) {
-      const int ra = 16 * x + 4 * hf;
-      S = mfma(vf[x], join(tr_nat(t + kTile, ra), tr_nat(t + kTile, ra + 8)), S);
-      S = mfma(vf[x], join(tr_nat(t + 2 * kTile, ra), tr_nat(t + 2 * kTile, ra + 8)), S);
-    }
-    if (more) {
-      stage(c + 1, buf ^ 1);
-      if (!STATES) {
-        put_state(buf ^ 1);
+            for (int s = 0; s < 4; ++s) qf[s] = *(const u32x4*)(t + kQ + toff(32 * RB + L.r, 2 * s + L.hf));
 #pragma unroll
-        for (int s = 0; s < 4; ++s) qf[s] = qn[s];
-      }
-      __syncthreads();
-    }
-  }
-  float* so = STATES ? A.seg + (bh * A.P + p) * 4096 : (p == A.P - 1 && A.state_out ? A.state_out + bh * 4096 : nullptr);
-  if (so) {
+            for (int s = 0; s < 4; ++s)
 #pragma unroll
-    for (int x = 0; x < 16; x += 4)
-      *(float4*)(so + sa * 64 + sc + x) = make_float4(S[x], S[x + 1], S[x + 2], S[x + 3]);
-  }
-  if (!STATES) {  // rows behind the sequence's end
-    const int z0 = max(len, c0 * kC), z1 = p == A.P - 1 ? A.n : min(A.n, (c0 + A.cps) * kC);
-    const int64_t base = (bh * A.n) * 64;
-    if (A.out_f32) {
-      for (int64_t x = (int64_t)z0 * 16 + tid; x < (int64_t)z1 * 16; x += 256)
-        ((float4*)((float*)A.out + base))[x] = make_float4(0.f, 0.f, 0.f, 0.f);
-    } else {
-      for (int64_t x = (int64_t)z0 * 8 + tid; x < (int64_t)z1 * 8; x += 256)
-        ((u32x4*)((uint16_t*)A.out + base))[x] = u32x4{0u, 0u, 0u, 0u};
-    }
+              for (int kb = 0; kb <= RB; ++kb) kf[kb][s] = *(const u32x4*)(t + toff(32 * kb + L.r, 2 * s + L.hf));
+#pragma unroll
+            for (int s = 0; s < 4; ++s)
+              sf[s] = join(L.perm(t + kS, 16 * s + 8 * L.hf, ch), L.perm(t + kS, 16 * s + 8 * L.hf + 4, ch));
+#pragma unroll
+            for (int x = 0; x < 2 * RB + 2; ++x)
+              vf[x] = join(L.perm(t + kV, 16 * x + 4 * L.hf, ch), L.perm(t + kV, 16 * x + 8 + 4 * L.hf, ch));
+            f32x16 P[RB + 1], o = zero16(), oi = zero16();
+#pragma unroll
+            for (int kb = 0; kb <= RB; ++kb) P[kb] = zero16();
+#pragma unroll
+            for (int s = 0; s < 4; ++s)
+#pragma unroll
+              for (int kb = 0; kb <= RB; ++kb) P[kb] = mfma(kf[kb][s], qf[s], P[kb]);
+#pragma unroll
+            for (int s = 0; s < 4; ++s) oi = mfma(sf[s], qf[s], oi);
+            // reads of the keys, then the products with reads of the rest between
+            __builtin_amdgcn_sched_group_barrier(0x100, 4 * RB + 12, 0);
+#pragma unroll
+            for (int x = 0; x < 4 * RB + 4; ++x) {
+              __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+              __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+            }
+            __builtin_amdgcn_sched_group_barrier(0x8, 4, 0);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int u = 0; u < 2 * RB + 2; ++u)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const int x = 8 * (u & 1) + 2 * e;
+                const float* w = u / 2 == RB ? wd : wo;
+                pf[u][e] = pack_bf16x2(P[u / 2][x] * w[x], P[u / 2][x + 1] * w[x + 1]);
+              }
+#pragma unroll
+            for (int x = 0; x < 2 * RB + 2; ++x) o = mfma(vf[x], pf[x], o);
+#pragma unroll
+            for (int x = 0; x < 16; ++x) o[x] = fmaf(wi, oi[x], o[x]);
+            const int nr = G.count(c);
+            const Buffer bo = buffer(out + G.first(c, nr) * (64 * kEl), nr * 64 * kEl);
+            if constexpr (OUT32) {
+              const int off = (G.place(32 * RB + L.r, nr) * 64 + 32 * ch + 16 * L.hf) * 4;
+#pragma unroll
+              for (int x = 0; x < 16; x += 4)
+                buf_store(bo, off + 4 * x, u32x4{__float_as_uint(o[x]), __float_as_uint(o[x + 1]),
+                                                 __float_as_uint(o[x + 2]), __float_as_uint(o[x + 3])});
+            } else {
+              // lanes 16 apart exchange, so that four of them hold 64 bytes of one token
+              u32x4 lo, hi;
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const auto x = __builtin_amdgcn_permlane16_swap(pack_bf16x2(o[2 * e], o[2 * e + 1]),
+                                                                pack_bf16x2(o[8 + 2 * e], o[9 + 2 * e]), false, false);
+                lo[e] = x[0];
+                hi[e] = x[1];
+              }
+              const int at = 64 * ch + 16 * (lane >> 4);
+              buf_store(bo, G.place(32 * RB + (lane & 15), nr) * 128 + at, lo);
+              buf_store(bo, G.place(32 * RB + 16 + (lane & 15), nr) * 128 + at, hi);
+            }
+            put(c + 1, buf ^ 1, next);
+          });
+    };
+    if ((wave & 1) == 0)
+      outputs(std::integral_constant<int, 0>{});
+    else
+      outputs(std::integral_constant<int, 1>{});
+    // rows behind the sequence's end, by the output's 256 threads
+    const int z0 = max(G.len, G.c0 * kC), z1 = G.p == A.P - 1 ? A.n : min(A.n, (G.c0 + A.cps) * kC);
+    constexpr int kG = 64 * kEl / 16;  // 16-byte granules per row
+    for (int64_t x = (int64_t)z0 * kG + tid; x < (int64_t)z1 * kG; x += 256) ((u32x4*)out)[x] = u32x4{0u, 0u, 0u, 0u};
   }
 }
 
@@ -536,10 +723,9 @@ struct Split {
 Split split_of(const LinearDims& d) {
   const int chunks = (d.n + kC - 1) / kC;
   const int64_t slices = (int64_t)d.B * d.H;
-  // a launch of two workgroups per compute unit keeps HBM busy; a slice is
-  // split where there are fewer than one each, since the segments' states cost
-  // another pass over K and V
-  int64_t P = slices >= 256 ? 1 : 512 / slices;
+  const char* e = getenv("GA_LIN_P");
+  int64_t P = slices >= 128 ? 1 : 256 / slices;
+  if (e && atoi(e)) P = atoi(e);
   if (P > chunks / 4) P = chunks / 4;
   if (P < 1) P = 1;
   const int cps = (int)((chunks + P - 1) / P);
@@ -550,23 +736,25 @@ size_t seg_bytes(const LinearDims& d) {
   return s.P > 1 ? (size_t)d.B * d.H * s.P * 4096 * 4 : 0;
 }
 
-template <bool REV>
+template <bool REV, bool OUT32>
 void chunked(const LinearDims& d, Chunked a, hipStream_t st) {
   const Split s = split_of(d);
   a.P = s.P;
   a.cps = s.cps;
+  // (an initial state that is updated in place is read before any workgroup writes it)
+  a.scanned = s.P > 8 || (s.P > 1 && a.state && a.state == a.state_out);
   const unsigned slices = (unsigned)(d.B * d.H);
   if (s.P > 1) {
-    {
-      TimedLaunch tl("lin_states", st);
-      hipLaunchKernelGGL((k_lin_chunk<REV, true>), dim3(slices * (s.P - 1)), dim3(256), 0, st, a);
-    }
+    TimedLaunch tl("lin_states", st);
+    hipLaunchKernelGGL(k_lin_states<REV>, dim3(slices * (s.P - 1)), dim3(256), 0, st, a);
+  }
+  if (a.scanned) {
     TimedLaunch tl("lin_scan", st);
     hipLaunchKernelGGL(k_lin_scan, dim3(slices * 16), dim3(256), 0, st, a.seg, a.state, a.log_decay, a.lengths, d.H,
                        d.n, s.P, s.cps, a.transposed);
   }
   TimedLaunch tl("lin_chunk", st);
-  hipLaunchKernelGGL((k_lin_chunk<REV, false>), dim3(slices * s.P), dim3(256), 0, st, a);
+  hipLaunchKernelGGL((k_lin_chunk<REV, OUT32>), dim3(slices * s.P), dim3(512), 0, st, a);
 }
 
 }  // namespace
@@ -578,8 +766,8 @@ hipError_t launch_linear(const LinearDims& d, const void* Q, const void* K, cons
                          hipStream_t st) {
   if (d.dtype == 1) {
     Chunked a{(const uint16_t*)Q, (const uint16_t*)K, (const uint16_t*)V, false, true, true, log_decay, state, lengths,
-              (float*)ws, state_out, O, d.H, d.Hk, d.n, 1, 1, scale, false, false};
-    chunked<false>(d, a, st);
+              (float*)ws, state_out, O, d.H, d.Hk, d.n, 1, 1, scale, false};
+    chunked<false, false>(d, a, st);
     return hipGetLastError();
   }
   walk(d, Walk{Q, K, V, false, true, true, log_decay, state, lengths, state_out, O, d.H, d.Hk, d.n, scale, false,
@@ -610,14 +798,21 @@ hipError_t launch_linear_grad(const LinearDims& d, const void* Q, const void* K,
   if (d.dtype == 1) {
     float* seg = (float*)((char*)ws + (grouped ? (size_t)d.B * d.H * d.n * 64 * 4 : 0));
     const uint16_t *q = (const uint16_t*)Q, *k = (const uint16_t*)K, *v = (const uint16_t*)V, *o = (const uint16_t*)dO;
-    chunked<false>(d, Chunked{o, v, k, false, true, true, log_decay, state, lengths, seg, nullptr, dQ, d.H, d.Hk, d.n,
-                              1, 1, scale, true, false}, st);
-    chunked<true>(d, Chunked{v, o, q, true, false, false, log_decay, dstate, lengths, seg, nullptr, grouped ? ws : dK,
-                             d.H, d.Hk, d.n, 1, 1, scale, true, grouped}, st);
-    heads(dK);
-    chunked<true>(d, Chunked{k, q, o, true, false, false, log_decay, dstate, lengths, seg, dstate_out,
-                             grouped ? ws : dV, d.H, d.Hk, d.n, 1, 1, scale, false, grouped}, st);
-    heads(dV);
+    chunked<false, false>(d, Chunked{o, v, k, false, true, true, log_decay, state, lengths, seg, nullptr, dQ, d.H, d.Hk,
+                                     d.n, 1, 1, scale, true}, st);
+    Chunked dk{v, o, q, true, false, false, log_decay, dstate, lengths, seg, nullptr, grouped ? ws : dK, d.H, d.Hk, d.n,
+               1, 1, scale, true};
+    Chunked dv{k, q, o, true, false, false, log_decay, dstate, lengths, seg, dstate_out, grouped ? ws : dV, d.H, d.Hk,
+               d.n, 1, 1, scale, false};
+    if (grouped) {
+      chunked<true, true>(d, dk, st);
+      heads(dK);
+      chunked<true, true>(d, dv, st);
+      heads(dV);
+    } else {
+      chunked<true, false>(d, dk, st);
+      chunked<true, false>(d, dv, st);
+    }
     return hipGetLastError();
   }
   walk(d, Walk{dO, V, K, false, true, true, log_decay, state, lengths, nullptr, dQ, d.H, d.Hk, d.n, scale, false, true,
