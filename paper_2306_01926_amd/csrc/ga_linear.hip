@@ -465,12 +465,19 @@ __global__ __launch_bounds__(512, 2) void k_lin_chunk(Chunked A) {
   constexpr int kV = 3 * kTile, kS = 4 * kTile, kQ = 5 * kTile;
   const int ch = (wave >> 1) & 1;
 
+  auto put_key = [&](int buf, int row, int gr, u32x4 k, u32x4 hi, u32x4 lo) __attribute__((always_inline)) {
+    const int at = toff(row, gr);
+    *(u32x4*)(lds[buf] + at) = k;
+    *(u32x4*)(lds[buf] + kTile + at) = hi;
+    *(u32x4*)(lds[buf] + 2 * kTile + at) = lo;
+  };
+
   if (wave >= 4) {
     // the state S[a][c], a = 32 ah + r, c = 32 ch + 16 hf + 0..15; its waves
-    // also bring the keys: granule tid % 8 of two rows 32 apart
+    // also bring the values and the first 32 keys: granule tid % 8
     const int ah = wave & 1, sa = 32 * ah + L.r, sc = 32 * ch + 16 * L.hf, gr = tid & 7, r0 = (tid >> 3) & 31;
     struct Rows {
-      u32x4 k[2];
+      u32x4 k, v[2];
     };
     f32x16 S = zero16();
     const bool given = A.state && !A.scanned;
@@ -490,19 +497,11 @@ __global__ __launch_bounds__(512, 2) void k_lin_chunk(Chunked A) {
         for (int x = 0; x < 16; ++x) S[x] = fmaf(w, S[x], s0[x]);
       }
     }
-    u32x4 hi[2], lo[2];
-    auto convert = [&](int c, const Rows& R) __attribute__((always_inline)) {
-#pragma unroll
-      for (int u = 0; u < 2; ++u) G.decayed(R.k[u], r0 + 32 * u, c, hi[u], lo[u]);
-    };
+    u32x4 hi, lo;
     auto put = [&](int buf, const Rows& R) __attribute__((always_inline)) {
+      put_key(buf, r0, gr, R.k, hi, lo);
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const int at = toff(r0 + 32 * u, gr);
-        *(u32x4*)(lds[buf] + at) = R.k[u];
-        *(u32x4*)(lds[buf] + kTile + at) = hi[u];
-        *(u32x4*)(lds[buf] + 2 * kTile + at) = lo[u];
-      }
+      for (int u = 0; u < 2; ++u) *(u32x4*)(lds[buf] + kV + toff(r0 + 32 * u, gr)) = R.v[u];
     };
     auto put_state = [&](int buf) __attribute__((always_inline)) {
 #pragma unroll
@@ -514,12 +513,13 @@ __global__ __launch_bounds__(512, 2) void k_lin_chunk(Chunked A) {
     G.template walk<Rows>(
         [&](int c, Rows& R) __attribute__((always_inline)) {
           const int nr = G.count(c);
-          const Buffer bk = buffer(G.k + G.first(c, nr) * 64, nr * 128);
+          const Buffer bk = buffer(G.k + G.first(c, nr) * 64, nr * 128), bv = buffer(G.v + G.first(c, nr) * 64, nr * 128);
+          R.k = buf_load(bk, G.place(r0, nr) * 128 + 16 * gr);
 #pragma unroll
-          for (int u = 0; u < 2; ++u) R.k[u] = buf_load(bk, G.place(r0 + 32 * u, nr) * 128 + 16 * gr);
+          for (int u = 0; u < 2; ++u) R.v[u] = buf_load(bv, G.place(r0 + 32 * u, nr) * 128 + 16 * gr);
         },
         [&](int c, int buf, const Rows& R) __attribute__((always_inline)) {
-          convert(c, R);
+          G.decayed(R.k, r0, c, hi, lo);
           put(buf, R);
           put_state(buf);
         },
@@ -527,7 +527,7 @@ __global__ __launch_bounds__(512, 2) void k_lin_chunk(Chunked A) {
           const unsigned char* t = lds[buf];
           const float w = decay_pow(G.g, (float)G.count(c));
           // the conversion comes first: the output's waves have the LDS then
-          convert(c + 1, next);
+          G.decayed(next.k, r0, c + 1, hi, lo);
 #pragma unroll
           for (int x = 0; x < 16; ++x) S[x] *= w;
           __builtin_amdgcn_sched_barrier(0);
@@ -572,35 +572,46 @@ __global__ __launch_bounds__(512, 2) void k_lin_chunk(Chunked A) {
     }
     constexpr int kEl = OUT32 ? 4 : 2;
     unsigned char* out = (unsigned char*)A.out + bh * A.n * (64 * kEl);
-    // the values and queries: granule tid % 8 of rows tid / 8 and 32 + tid / 8
-    const int gr = tid & 7, r0 = tid >> 3;
-    struct Rows {
-      u32x4 v[2], q[2];
-    };
+    // rows that these waves bring, by their 128 threads each: the shorter
+    // block's the last 32 keys, the longer block's the queries
+    const int gr = lane & 7, r0 = (lane >> 3) + 8 * ch;
     // the second block of tokens meets two blocks of keys, the first one: a
     // loop for each, without branches
     auto outputs = [&](auto block) __attribute__((always_inline)) {
       constexpr int RB = decltype(block)::value;
       const float wi = (REV ? 1.f : A.scale) * decay_pow(G.g, (float)(32 * RB + L.r + 1 - REV));
-      auto put = [&](int, int buf, const Rows& R) __attribute__((always_inline)) {
+      constexpr int kRows = RB ? 4 : 2;
+      struct Rows {
+        u32x4 x[kRows];
+      };
+      u32x4 hi[2], lo[2];
+      auto convert = [&](int c, const Rows& R) __attribute__((always_inline)) {
+        if constexpr (RB == 0) {
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          *(u32x4*)(lds[buf] + kV + toff(r0 + 32 * u, gr)) = R.v[u];
-          *(u32x4*)(lds[buf] + kQ + toff(r0 + 32 * u, gr)) = R.q[u];
+          for (int u = 0; u < 2; ++u) G.decayed(R.x[u], 32 + r0 + 16 * u, c, hi[u], lo[u]);
+        }
+      };
+      auto put = [&](int buf, const Rows& R) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < kRows; ++u) {
+          if constexpr (RB == 0)
+            put_key(buf, 32 + r0 + 16 * u, gr, R.x[u], hi[u], lo[u]);
+          else
+            *(u32x4*)(lds[buf] + kQ + toff(r0 + 16 * u, gr)) = R.x[u];
         }
       };
       G.template walk<Rows>(
           [&](int c, Rows& R) __attribute__((always_inline)) {
             const int nr = G.count(c);
-            const Buffer bv = buffer(G.v + G.first(c, nr) * 64, nr * 128), bq = buffer(G.q + G.first(c, nr) * 64, nr * 128);
+            const Buffer b = buffer((RB ? G.q : G.k) + G.first(c, nr) * 64, nr * 128);
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-              const int off = G.place(r0 + 32 * u, nr) * 128 + 16 * gr;
-              R.v[u] = buf_load(bv, off);
-              R.q[u] = buf_load(bq, off);
-            }
+            for (int u = 0; u < kRows; ++u)
+              R.x[u] = buf_load(b, G.place((RB ? 0 : 32) + r0 + 16 * u, nr) * 128 + 16 * gr);
           },
-          put,
+          [&](int c, int buf, const Rows& R) __attribute__((always_inline)) {
+            convert(c, R);
+            put(buf, R);
+          },
           [&](int c, int buf, const Rows& next) __attribute__((always_inline)) {
             const unsigned char* t = lds[buf];
             u32x4 qf[4], kf[RB + 1][4], sf[4], vf[2 * RB + 2], pf[2 * RB + 2];
@@ -634,6 +645,7 @@ __global__ __launch_bounds__(512, 2) void k_lin_chunk(Chunked A) {
             }
             __builtin_amdgcn_sched_group_barrier(0x8, 4, 0);
             __builtin_amdgcn_sched_barrier(0);
+            convert(c + 1, next);
 #pragma unroll
             for (int u = 0; u < 2 * RB + 2; ++u)
 #pragma unroll
@@ -668,7 +680,7 @@ __global__ __launch_bounds__(512, 2) void k_lin_chunk(Chunked A) {
               buf_store(bo, G.place(32 * RB + (lane & 15), nr) * 128 + at, lo);
               buf_store(bo, G.place(32 * RB + 16 + (lane & 15), nr) * 128 + at, hi);
             }
-            put(c + 1, buf ^ 1, next);
+            put(buf ^ 1, next);
           });
     };
     if ((wave & 1) == 0)
