@@ -15,7 +15,6 @@
 
 #include <float.h>
 #include <stdint.h>
-#include <stdlib.h>
 
 #include <type_traits>
 
@@ -278,13 +277,13 @@ __device__ __forceinline__ void buf_store(Buffer b, int off, u32x4 x) {
 }
 
 struct Chunked {
-  const uint16_t *q, *k, *v;          // roles (see the head of the file)
-  bool q_shared, k_shared, v_shared;  // the tensor has Hk heads
+  const uint16_t *q, *k, *v, *w;                // roles (see the head of the file; w: k_lin_grad alone)
+  bool q_shared, k_shared, v_shared, w_shared;  // the tensor has Hk heads
   const float *log_decay, *state;
   const int32_t* lengths;
   float* seg;        // [B H][P][64][64]: the segments' local states, or (scanned) the states before them; P > 1 only
   float* state_out;
-  void* out;
+  void *out, *out2;
   int H, Hk, n, P, cps;  // segments per slice, chunks per segment
   float scale;
   bool transposed, scanned;
@@ -297,7 +296,7 @@ struct Chunked {
 // the sum, and the scale sits in the sum.
 template <bool REV>
 struct Segment {
-  const uint16_t *q, *k, *v;
+  const uint16_t *q, *k, *v, *w;
   int64_t bh;
   int p, len, c0, c1;
   float g, ks;
@@ -309,6 +308,7 @@ struct Segment {
     q = A.q + (A.q_shared ? bk : bh) * A.n * 64;
     k = A.k + (A.k_shared ? bk : bh) * A.n * 64;
     v = A.v + (A.v_shared ? bk : bh) * A.n * 64;
+    w = A.w + (A.w_shared ? bk : bh) * A.n * 64;
     g = decay_log2(A.log_decay[h]);
     ks = REV ? A.scale : 1.f;
     c0 = p * A.cps;
@@ -383,11 +383,37 @@ struct Lanes {
   }
 };
 
+// Features 32 half .. of 32 tokens from walk row x0, lane (r, hf) holding
+// features 16 hf + 0..15 of token r, into the chunk's buffer.
+template <bool OUT32, bool REV>
+__device__ __forceinline__ void store_tokens(Buffer b, const Segment<REV>& G, int x0, int nr, int half, int lane,
+                                             const f32x16& o) {
+  if constexpr (OUT32) {
+    const int off = (G.place(x0 + (lane & 31), nr) * 64 + 32 * half + 16 * (lane >> 5)) * 4;
+#pragma unroll
+    for (int x = 0; x < 16; x += 4)
+      buf_store(b, off + 4 * x, u32x4{__float_as_uint(o[x]), __float_as_uint(o[x + 1]), __float_as_uint(o[x + 2]),
+                                      __float_as_uint(o[x + 3])});
+  } else {
+    // lanes 16 apart exchange, so that four of them hold 64 bytes of one token
+    u32x4 lo, hi;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const auto x = __builtin_amdgcn_permlane16_swap(pack_bf16x2(o[2 * e], o[2 * e + 1]),
+                                                      pack_bf16x2(o[8 + 2 * e], o[9 + 2 * e]), false, false);
+      lo[e] = x[0];
+      hi[e] = x[1];
+    }
+    const int at = 64 * half + 16 * (lane >> 4);
+    buf_store(b, G.place(x0 + (lane & 15), nr) * 128 + at, lo);
+    buf_store(b, G.place(x0 + 16 + (lane & 15), nr) * 128 + at, hi);
+  }
+}
+
 // The local states of the segments but the last, from zero: four waves, a
-// quadrant of the state each.  grid: slices (P - 1).
+// quadrant of the state each.
 template <bool REV>
-__global__ __launch_bounds__(256, 3) void k_lin_states(Chunked A) {
-  __shared__ __attribute__((aligned(16))) unsigned char lds[2][3 * kTile];  // V, K hi, K lo (decayed)
+__device__ __forceinline__ void local_states(const Chunked& A, unsigned char (*lds)[3 * kTile]) {
   const int64_t bh = blockIdx.x / (A.P - 1);
   const Segment<REV> G(A, bh, (int)(blockIdx.x - bh * (A.P - 1)));
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -449,14 +475,20 @@ __global__ __launch_bounds__(256, 3) void k_lin_states(Chunked A) {
   for (int x = 0; x < 16; x += 4) *(float4*)(so + x) = make_float4(S[x], S[x + 1], S[x + 2], S[x + 3]);
 }
 
-// Outputs (and the final state).  OUT32: the output is fp32 (a query head's
-// share of a shared head's gradient).  grid: slices P.
-template <bool REV, bool OUT32>
-__global__ __launch_bounds__(512, 2) void k_lin_chunk(Chunked A) {
-  constexpr int kBuf = 6 * kTile;  // K, K hi, K lo (decayed), V, the state, Q
-  __shared__ __attribute__((aligned(16))) unsigned char lds[2][kBuf];
-  const int64_t bh = blockIdx.x / A.P;
-  const Segment<REV> G(A, bh, (int)(blockIdx.x - bh * A.P));
+// grid (slices (P - 1), directions): a gradient needs the states of both walks.
+__global__ __launch_bounds__(256, 3) void k_lin_states(Chunked F, Chunked B) {
+  __shared__ __attribute__((aligned(16))) unsigned char lds[2][3 * kTile];  // V, K hi, K lo (decayed)
+  if (blockIdx.y == 0)
+    local_states<false>(F, lds);
+  else
+    local_states<true>(B, lds);
+}
+
+// Outputs of a forward walk (and the final state): workgroup `block` of slices P.
+constexpr int kForwardBuf = 6 * kTile;  // K, K hi, K lo (decayed), V, the state, Q
+__device__ __forceinline__ void forward_walk(const Chunked& A, int block, unsigned char (*lds)[kForwardBuf]) {
+  const int64_t bh = block / A.P;
+  const Segment<false> G(A, bh, (int)(block - bh * A.P));
   // the wave's index is scalar, so that branches on it are jumps: matrix
   // instructions do not heed the lane mask
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -570,8 +602,7 @@ __global__ __launch_bounds__(512, 2) void k_lin_chunk(Chunked A) {
       wd[x] = d >= 0 ? A.scale * decay_pow(G.g, (float)d) : 0.f;
       wo[x] = A.scale * decay_pow(G.g, (float)(32 + d));
     }
-    constexpr int kEl = OUT32 ? 4 : 2;
-    unsigned char* out = (unsigned char*)A.out + bh * A.n * (64 * kEl);
+    unsigned char* out = (unsigned char*)A.out + bh * A.n * 128;
     // rows that these waves bring, by their 128 threads each: the shorter
     // block's the last 32 keys, the longer block's the queries
     const int gr = lane & 7, r0 = (lane >> 3) + 8 * ch;
@@ -579,7 +610,7 @@ __global__ __launch_bounds__(512, 2) void k_lin_chunk(Chunked A) {
     // loop for each, without branches
     auto outputs = [&](auto block) __attribute__((always_inline)) {
       constexpr int RB = decltype(block)::value;
-      const float wi = (REV ? 1.f : A.scale) * decay_pow(G.g, (float)(32 * RB + L.r + 1 - REV));
+      const float wi = A.scale * decay_pow(G.g, (float)(32 * RB + L.r + 1));
       constexpr int kRows = RB ? 4 : 2;
       struct Rows {
         u32x4 x[kRows];
@@ -659,27 +690,8 @@ __global__ __launch_bounds__(512, 2) void k_lin_chunk(Chunked A) {
 #pragma unroll
             for (int x = 0; x < 16; ++x) o[x] = fmaf(wi, oi[x], o[x]);
             const int nr = G.count(c);
-            const Buffer bo = buffer(out + G.first(c, nr) * (64 * kEl), nr * 64 * kEl);
-            if constexpr (OUT32) {
-              const int off = (G.place(32 * RB + L.r, nr) * 64 + 32 * ch + 16 * L.hf) * 4;
-#pragma unroll
-              for (int x = 0; x < 16; x += 4)
-                buf_store(bo, off + 4 * x, u32x4{__float_as_uint(o[x]), __float_as_uint(o[x + 1]),
-                                                 __float_as_uint(o[x + 2]), __float_as_uint(o[x + 3])});
-            } else {
-              // lanes 16 apart exchange, so that four of them hold 64 bytes of one token
-              u32x4 lo, hi;
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                const auto x = __builtin_amdgcn_permlane16_swap(pack_bf16x2(o[2 * e], o[2 * e + 1]),
-                                                                pack_bf16x2(o[8 + 2 * e], o[9 + 2 * e]), false, false);
-                lo[e] = x[0];
-                hi[e] = x[1];
-              }
-              const int at = 64 * ch + 16 * (lane >> 4);
-              buf_store(bo, G.place(32 * RB + (lane & 15), nr) * 128 + at, lo);
-              buf_store(bo, G.place(32 * RB + 16 + (lane & 15), nr) * 128 + at, hi);
-            }
+            const Buffer bo = buffer(out + G.first(c, nr) * 128, nr * 128);
+            store_tokens<false>(bo, G, 32 * RB, nr, ch, lane, o);
             put(buf ^ 1, next);
           });
     };
@@ -689,31 +701,239 @@ __global__ __launch_bounds__(512, 2) void k_lin_chunk(Chunked A) {
       outputs(std::integral_constant<int, 1>{});
     // rows behind the sequence's end, by the output's 256 threads
     const int z0 = max(G.len, G.c0 * kC), z1 = G.p == A.P - 1 ? A.n : min(A.n, (G.c0 + A.cps) * kC);
-    constexpr int kG = 64 * kEl / 16;  // 16-byte granules per row
-    for (int64_t x = (int64_t)z0 * kG + tid; x < (int64_t)z1 * kG; x += 256) ((u32x4*)out)[x] = u32x4{0u, 0u, 0u, 0u};
+    for (int64_t x = (int64_t)z0 * 8 + tid; x < (int64_t)z1 * 8; x += 256) ((u32x4*)out)[x] = u32x4{0u, 0u, 0u, 0u};
   }
+}
+
+// The gradients of K and V in one backward walk: dV has the roles q = K, k = Q,
+// v = dO, dK the roles q = V (w), k = dO, v = Q, and both meet the same state
+// R[a][c] (a: feature of q and k, c: of v and dO), dK with its other side.
+// Eight waves: waves 0-3 form 32 tokens by 64 features of dV (0, 1) or dK
+// (2, 3), waves 4-7 the state.  out: dV, out2: dK; OUT32: they are fp32 (a
+// query head's share of a shared head's gradient).
+constexpr int kBackwardBuf = 7 * kTile;  // Q, Q hi, Q lo (decayed), dO, K, V, the state
+template <bool OUT32>
+__device__ __forceinline__ void backward_walk(const Chunked& A, int block, unsigned char (*lds)[kBackwardBuf]) {
+  constexpr int kQ = 0, kO = 3 * kTile, kK = 4 * kTile, kV = 5 * kTile, kS = 6 * kTile;
+  const int64_t bh = block / A.P;
+  const Segment<true> G(A, bh, (int)(block - bh * A.P));
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lane = tid & 63;
+  const Lanes L(lane);
+
+  // every thread brings granule tid % 8 of row tid / 8 of the four tensors
+  struct Rows {
+    u32x4 k, v, q, w;
+  };
+  const int gr = tid & 7, r0 = tid >> 3, at = toff(r0, gr);
+  u32x4 hi, lo;
+  auto load = [&](int c, Rows& R) __attribute__((always_inline)) {
+    const int nr = G.count(c);
+    const int64_t f = G.first(c, nr) * 64;
+    const int off = G.place(r0, nr) * 128 + 16 * gr;
+    R.k = buf_load(buffer(G.k + f, nr * 128), off);
+    R.v = buf_load(buffer(G.v + f, nr * 128), off);
+    R.q = buf_load(buffer(G.q + f, nr * 128), off);
+    R.w = buf_load(buffer(G.w + f, nr * 128), off);
+  };
+  auto put = [&](int buf, const Rows& R) __attribute__((always_inline)) {
+    unsigned char* t = lds[buf] + at;
+    *(u32x4*)(t + kQ) = R.k;
+    *(u32x4*)(t + kQ + kTile) = hi;
+    *(u32x4*)(t + kQ + 2 * kTile) = lo;
+    *(u32x4*)(t + kO) = R.v;
+    *(u32x4*)(t + kK) = R.q;
+    *(u32x4*)(t + kV) = R.w;
+  };
+
+  if (wave >= 4) {
+    const int ah = wave & 1, ch = (wave >> 1) & 1, sa = 32 * ah + L.r, sc = 32 * ch + 16 * L.hf;
+    f32x16 S = zero16();
+    const float* s0 = A.scanned ? A.seg + (bh * A.P + G.p) * 4096 : (A.state ? A.state + bh * 4096 : nullptr);
+    if (s0) {
+#pragma unroll
+      for (int x = 0; x < 16; ++x) S[x] = s0[sa * 64 + sc + x];
+    }
+    if (!A.scanned) {
+      for (int u = 0; u < G.p; ++u) {
+        const float w = decay_pow(G.g, G.tokens(A, u));
+        const float* s1 = A.seg + (bh * A.P + u) * 4096 + sa * 64 + sc;
+#pragma unroll
+        for (int x = 0; x < 16; ++x) S[x] = fmaf(w, S[x], s1[x]);
+      }
+    }
+    auto put_state = [&](int buf) __attribute__((always_inline)) {
+#pragma unroll
+      for (int x = 0; x < 16; x += 8)
+        *(u32x4*)(lds[buf] + kS + toff(sa, 4 * ch + 2 * L.hf + x / 8)) =
+            u32x4{pack_bf16x2(S[x], S[x + 1]), pack_bf16x2(S[x + 2], S[x + 3]), pack_bf16x2(S[x + 4], S[x + 5]),
+                  pack_bf16x2(S[x + 6], S[x + 7])};
+    };
+    G.template walk<Rows>(
+        load,
+        [&](int c, int buf, const Rows& R) __attribute__((always_inline)) {
+          G.decayed(R.k, r0, c, hi, lo);
+          put(buf, R);
+          put_state(buf);
+        },
+        [&](int c, int buf, const Rows& next) __attribute__((always_inline)) {
+          const unsigned char* t = lds[buf];
+          const float w = decay_pow(G.g, (float)G.count(c));
+          G.decayed(next.k, r0, c + 1, hi, lo);
+#pragma unroll
+          for (int x = 0; x < 16; ++x) S[x] *= w;
+          __builtin_amdgcn_sched_barrier(0);
+          u32x4 vf[4], kh[4], kl[4];
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            const int ra = 16 * x + 4 * L.hf;
+            vf[x] = join(L.perm(t + kO, ra, ch), L.perm(t + kO, ra + 8, ch));
+            kh[x] = join(L.nat(t + kQ + kTile, ra, ah), L.nat(t + kQ + kTile, ra + 8, ah));
+            kl[x] = join(L.nat(t + kQ + 2 * kTile, ra, ah), L.nat(t + kQ + 2 * kTile, ra + 8, ah));
+          }
+          f32x16 T = zero16();
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            S = mfma(vf[x], kh[x], S);
+            T = mfma(vf[x], kl[x], T);
+          }
+          put(buf ^ 1, next);
+#pragma unroll
+          for (int x = 0; x < 16; ++x) S[x] += T[x];
+          put_state(buf ^ 1);
+        });
+    if (G.p == A.P - 1 && A.state_out) {
+      float* so = A.state_out + bh * 4096 + sa * 64 + sc;
+#pragma unroll
+      for (int x = 0; x < 16; x += 4) *(float4*)(so + x) = make_float4(S[x], S[x + 1], S[x + 2], S[x + 3]);
+    }
+  } else {
+    float wd[16], wo[16];  // decays inside a block of 32 tokens, and between two
+#pragma unroll
+    for (int x = 0; x < 16; ++x) {
+      const int d = L.r - (8 * (x / 4) + 4 * L.hf + x % 4);
+      wd[x] = d >= 0 ? A.scale * decay_pow(G.g, (float)d) : 0.f;
+      wo[x] = A.scale * decay_pow(G.g, (float)(32 + d));
+    }
+    const bool keys = wave >= 2;  // dK
+    const int tq = keys ? kV : kK, tk = keys ? kO : kQ, tv = keys ? kQ : kO;
+    constexpr int kEl = OUT32 ? 4 : 2;
+    unsigned char* out = (unsigned char*)(keys ? A.out2 : A.out) + bh * A.n * (64 * kEl);
+    // row of the state whose features a are the result's rows, permuted as L.perm does
+    const int prow = 16 * ((L.r >> 2) & 1) + 4 * (L.r >> 3) + (L.r & 3);
+    auto outputs = [&](auto block) __attribute__((always_inline)) {
+      constexpr int RB = decltype(block)::value;
+      const float wi = decay_pow(G.g, (float)(32 * RB + L.r));
+      G.template walk<Rows>(
+          load,
+          [&](int c, int buf, const Rows& R) __attribute__((always_inline)) {
+            G.decayed(R.k, r0, c, hi, lo);
+            put(buf, R);
+          },
+          [&](int c, int buf, const Rows& next) __attribute__((always_inline)) {
+            const unsigned char* t = lds[buf];
+            u32x4 qf[4], pf[2 * RB + 2];
+#pragma unroll
+            for (int s = 0; s < 4; ++s) qf[s] = *(const u32x4*)(t + tq + toff(32 * RB + L.r, 2 * s + L.hf));
+            f32x16 P[RB + 1], o[2] = {zero16(), zero16()};
+#pragma unroll
+            for (int kb = 0; kb <= RB; ++kb) P[kb] = zero16();
+#pragma unroll
+            for (int s = 0; s < 4; ++s)
+#pragma unroll
+              for (int kb = 0; kb <= RB; ++kb)
+                P[kb] = mfma(*(const u32x4*)(t + tk + toff(32 * kb + L.r, 2 * s + L.hf)), qf[s], P[kb]);
+            if (keys) {
+#pragma unroll
+              for (int s = 0; s < 4; ++s)
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+                  o[e] = mfma(*(const u32x4*)(t + kS + toff(32 * e + prow, 2 * s + L.hf)), qf[s], o[e]);
+            } else {
+#pragma unroll
+              for (int s = 0; s < 4; ++s)
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+                  o[e] = mfma(join(L.perm(t + kS, 16 * s + 8 * L.hf, e), L.perm(t + kS, 16 * s + 8 * L.hf + 4, e)),
+                              qf[s], o[e]);
+            }
+            G.decayed(next.k, r0, c + 1, hi, lo);
+#pragma unroll
+            for (int u = 0; u < 2 * RB + 2; ++u)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const int x = 8 * (u & 1) + 2 * e;
+                const float* w = u / 2 == RB ? wd : wo;
+                pf[u][e] = pack_bf16x2(P[u / 2][x] * w[x], P[u / 2][x + 1] * w[x + 1]);
+              }
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+#pragma unroll
+              for (int x = 0; x < 16; ++x) o[e][x] *= wi;
+#pragma unroll
+            for (int x = 0; x < 2 * RB + 2; ++x)
+#pragma unroll
+              for (int e = 0; e < 2; ++e)
+                o[e] = mfma(join(L.perm(t + tv, 16 * x + 4 * L.hf, e), L.perm(t + tv, 16 * x + 8 + 4 * L.hf, e)), pf[x],
+                            o[e]);
+            put(buf ^ 1, next);
+            const int nr = G.count(c);
+            const Buffer bo = buffer(out + G.first(c, nr) * (64 * kEl), nr * 64 * kEl);
+#pragma unroll
+            for (int e = 0; e < 2; ++e) store_tokens<OUT32>(bo, G, 32 * RB, nr, e, lane, o[e]);
+          });
+    };
+    if ((wave & 1) == 0)
+      outputs(std::integral_constant<int, 0>{});
+    else
+      outputs(std::integral_constant<int, 1>{});
+    // rows behind the sequence's end, by the 128 threads of each output
+    const int z0 = max(G.len, G.c0 * kC), z1 = G.p == A.P - 1 ? A.n : min(A.n, (G.c0 + A.cps) * kC);
+    constexpr int kG = 64 * kEl / 16;  // 16-byte granules per row
+    for (int64_t x = (int64_t)z0 * kG + (tid & 127); x < (int64_t)z1 * kG; x += 128)
+      ((u32x4*)out)[x] = u32x4{0u, 0u, 0u, 0u};
+  }
+}
+
+// grid: slices P.
+__global__ __launch_bounds__(512, 2) void k_lin_forward(Chunked A) {
+  __shared__ __attribute__((aligned(16))) unsigned char lds[2][kForwardBuf];
+  forward_walk(A, blockIdx.x, lds);
+}
+
+// dQ (the forward walk F) and dK, dV (the backward walk B) side by side: they
+// share no result, and one launch of both fills the compute units where one of
+// them would not.  grid: slices (B.P + F.P), the longer backward walks first.
+template <bool OUT32>
+__global__ __launch_bounds__(512, 2) void k_lin_backward(Chunked F, Chunked B, int backward) {
+  __shared__ __attribute__((aligned(16))) unsigned char lds[2 * kBackwardBuf];
+  if ((int)blockIdx.x < backward)
+    backward_walk<OUT32>(B, blockIdx.x, (unsigned char(*)[kBackwardBuf])lds);
+  else
+    forward_walk(F, blockIdx.x - backward, (unsigned char(*)[kForwardBuf])lds);
 }
 
 // Local states of the segments to the states before them, in place:
 // s_0 = the initial state, s_{p+1} = l^(tokens of p) s_p + local_p.
-__global__ __launch_bounds__(256) void k_lin_scan(float* seg, const float* state, const float* log_decay,
-                                                  const int32_t* lengths, int H, int n, int P, int cps,
-                                                  bool transposed) {
+// grid (slices 16, directions).
+__global__ __launch_bounds__(256) void k_lin_scan(Chunked F, Chunked B) {
+  const Chunked& A = blockIdx.y == 0 ? F : B;
+  if (!A.scanned) return;
   const int64_t bh = blockIdx.x >> 4;
   const int e = (blockIdx.x & 15) * 256 + threadIdx.x;
-  const float g = decay_log2(log_decay[bh % H]);
-  const int len = length_of(lengths, bh / H, n);
-  float s = !state ? 0.f : state[bh * 4096 + (transposed ? (e & 63) * 64 + (e >> 6) : e)];
-  float* at = seg + bh * P * 4096 + e;
-  for (int p0 = 0; p0 < P; p0 += 8) {
+  const float g = decay_log2(A.log_decay[bh % A.H]);
+  const int len = length_of(A.lengths, bh / A.H, A.n);
+  float s = !A.state ? 0.f : A.state[bh * 4096 + (A.transposed ? (e & 63) * 64 + (e >> 6) : e)];
+  float* at = A.seg + bh * A.P * 4096 + e;
+  for (int p0 = 0; p0 < A.P; p0 += 8) {
     float local[8];
 #pragma unroll
-    for (int u = 0; u < 8; ++u) local[u] = p0 + u < P - 1 ? at[(int64_t)(p0 + u) * 4096] : 0.f;
+    for (int u = 0; u < 8; ++u) local[u] = p0 + u < A.P - 1 ? at[(int64_t)(p0 + u) * 4096] : 0.f;
 #pragma unroll
     for (int u = 0; u < 8; ++u) {
-      if (p0 + u >= P) break;
+      if (p0 + u >= A.P) break;
       at[(int64_t)(p0 + u) * 4096] = s;
-      const int64_t tokens = min((int64_t)max(len - (int64_t)(p0 + u) * cps * kC, (int64_t)0), (int64_t)cps * kC);
+      const int64_t tokens = min(max((int64_t)len - (int64_t)(p0 + u) * A.cps * kC, (int64_t)0), (int64_t)A.cps * kC);
       s = fmaf(decay_pow(g, (float)tokens), s, local[u]);
     }
   }
@@ -732,54 +952,62 @@ void walk(const LinearDims& d, const Walk& w, hipStream_t st) {
 struct Split {
   int P, cps;
 };
-Split split_of(const LinearDims& d) {
+// A slice is split only where the walks would not fill half of the compute
+// units: HBM serves the others' reads as fast, and the segments' states cost
+// another pass over two of the tensors (B H = 128, n = 8000: 121 us whole, 137
+// in two; B H = 32, n = 20000: 284 us whole, 87 in eight).  Four chunks at
+// least to a segment.
+Split split_of(const LinearDims& d, int walks) {
   const int chunks = (d.n + kC - 1) / kC;
-  const int64_t slices = (int64_t)d.B * d.H;
-  const char* e = getenv("GA_LIN_P");
-  int64_t P = slices >= 128 ? 1 : 256 / slices;
-  if (e && atoi(e)) P = atoi(e);
+  const int64_t all = (int64_t)d.B * d.H * walks;
+  int64_t P = all >= 128 ? 1 : 256 / all;
   if (P > chunks / 4) P = chunks / 4;
   if (P < 1) P = 1;
   const int cps = (int)((chunks + P - 1) / P);
   return Split{(chunks + cps - 1) / cps, cps};
 }
-size_t seg_bytes(const LinearDims& d) {
-  const Split s = split_of(d);
+size_t seg_bytes(const LinearDims& d, Split s) {
   return s.P > 1 ? (size_t)d.B * d.H * s.P * 4096 * 4 : 0;
 }
 
-template <bool REV, bool OUT32>
-void chunked(const LinearDims& d, Chunked a, hipStream_t st) {
-  const Split s = split_of(d);
+void set_split(Chunked& a, Split s) {
   a.P = s.P;
   a.cps = s.cps;
   // (an initial state that is updated in place is read before any workgroup writes it)
   a.scanned = s.P > 8 || (s.P > 1 && a.state && a.state == a.state_out);
+}
+
+// The states before the segments of one walk, or of the two of a gradient.
+void segment_states(const LinearDims& d, const Chunked& f, const Chunked& b, unsigned directions, hipStream_t st) {
   const unsigned slices = (unsigned)(d.B * d.H);
-  if (s.P > 1) {
+  if (f.P > 1) {
     TimedLaunch tl("lin_states", st);
-    hipLaunchKernelGGL(k_lin_states<REV>, dim3(slices * (s.P - 1)), dim3(256), 0, st, a);
+    hipLaunchKernelGGL(k_lin_states, dim3(slices * (f.P - 1), directions), dim3(256), 0, st, f, b);
   }
-  if (a.scanned) {
+  if (f.scanned || b.scanned) {
     TimedLaunch tl("lin_scan", st);
-    hipLaunchKernelGGL(k_lin_scan, dim3(slices * 16), dim3(256), 0, st, a.seg, a.state, a.log_decay, a.lengths, d.H,
-                       d.n, s.P, s.cps, a.transposed);
+    hipLaunchKernelGGL(k_lin_scan, dim3(slices * 16, directions), dim3(256), 0, st, f, b);
   }
-  TimedLaunch tl("lin_chunk", st);
-  hipLaunchKernelGGL((k_lin_chunk<REV, OUT32>), dim3(slices * s.P), dim3(512), 0, st, a);
 }
 
 }  // namespace
 
-size_t linear_workspace(const LinearDims& d) { return d.dtype == 1 ? seg_bytes(d) : 0; }
+size_t linear_workspace(const LinearDims& d) { return d.dtype == 1 ? seg_bytes(d, split_of(d, 1)) : 0; }
 
 hipError_t launch_linear(const LinearDims& d, const void* Q, const void* K, const void* V, const float* log_decay,
                          const int32_t* lengths, const float* state, float scale, void* O, float* state_out, void* ws,
                          hipStream_t st) {
   if (d.dtype == 1) {
-    Chunked a{(const uint16_t*)Q, (const uint16_t*)K, (const uint16_t*)V, false, true, true, log_decay, state, lengths,
-              (float*)ws, state_out, O, d.H, d.Hk, d.n, 1, 1, scale, false};
-    chunked<false, false>(d, a, st);
+    Chunked a{};
+    a.q = (const uint16_t*)Q, a.k = (const uint16_t*)K, a.v = (const uint16_t*)V;
+    a.k_shared = a.v_shared = true;
+    a.log_decay = log_decay, a.state = state, a.lengths = lengths;
+    a.seg = (float*)ws, a.state_out = state_out, a.out = O;
+    a.H = d.H, a.Hk = d.Hk, a.n = d.n, a.scale = scale;
+    set_split(a, split_of(d, 1));
+    segment_states(d, a, Chunked{}, 1, st);
+    TimedLaunch tl("lin_forward", st);
+    hipLaunchKernelGGL(k_lin_forward, dim3((unsigned)(d.B * d.H * a.P)), dim3(512), 0, st, a);
     return hipGetLastError();
   }
   walk(d, Walk{Q, K, V, false, true, true, log_decay, state, lengths, state_out, O, d.H, d.Hk, d.n, scale, false,
@@ -788,7 +1016,8 @@ hipError_t launch_linear(const LinearDims& d, const void* Q, const void* K, cons
 }
 
 size_t linear_grad_workspace(const LinearDims& d) {
-  return (d.H == d.Hk ? 0 : (size_t)d.B * d.H * d.n * 64 * 4) + (d.dtype == 1 ? seg_bytes(d) : 0);
+  const size_t part = d.H == d.Hk ? 0 : (size_t)d.B * d.H * d.n * 64 * 4;  // a query head's share of dK or dV
+  return d.dtype == 1 ? 2 * part + 2 * seg_bytes(d, split_of(d, 2)) : part;
 }
 
 hipError_t launch_linear_grad(const LinearDims& d, const void* Q, const void* K, const void* V, const void* dO,
@@ -797,44 +1026,55 @@ hipError_t launch_linear_grad(const LinearDims& d, const void* Q, const void* K,
   const bool grouped = d.H != d.Hk;
   const int64_t row4 = (int64_t)d.n * 16, total4 = (int64_t)d.B * d.Hk * row4;
   const unsigned grid = (unsigned)((total4 + 255) / 256 < 8192 ? (total4 + 255) / 256 : 8192);
-  auto heads = [&](void* out) {
+  auto heads = [&](const void* part, void* out) {
     if (!grouped) return;
     TimedLaunch tl("lin_heads", st);
     if (d.dtype == 1)
-      hipLaunchKernelGGL(k_lin_heads<BF16>, dim3(grid), dim3(256), 0, st, (const float*)ws, d.H, d.Hk, row4, total4,
+      hipLaunchKernelGGL(k_lin_heads<BF16>, dim3(grid), dim3(256), 0, st, (const float*)part, d.H, d.Hk, row4, total4,
                          (uint16_t*)out);
     else
-      hipLaunchKernelGGL(k_lin_heads<F32>, dim3(grid), dim3(256), 0, st, (const float*)ws, d.H, d.Hk, row4, total4,
+      hipLaunchKernelGGL(k_lin_heads<F32>, dim3(grid), dim3(256), 0, st, (const float*)part, d.H, d.Hk, row4, total4,
                          (float*)out);
   };
   if (d.dtype == 1) {
-    float* seg = (float*)((char*)ws + (grouped ? (size_t)d.B * d.H * d.n * 64 * 4 : 0));
-    const uint16_t *q = (const uint16_t*)Q, *k = (const uint16_t*)K, *v = (const uint16_t*)V, *o = (const uint16_t*)dO;
-    chunked<false, false>(d, Chunked{o, v, k, false, true, true, log_decay, state, lengths, seg, nullptr, dQ, d.H, d.Hk,
-                                     d.n, 1, 1, scale, true}, st);
-    Chunked dk{v, o, q, true, false, false, log_decay, dstate, lengths, seg, nullptr, grouped ? ws : dK, d.H, d.Hk, d.n,
-               1, 1, scale, true};
-    Chunked dv{k, q, o, true, false, false, log_decay, dstate, lengths, seg, dstate_out, grouped ? ws : dV, d.H, d.Hk,
-               d.n, 1, 1, scale, false};
-    if (grouped) {
-      chunked<true, true>(d, dk, st);
-      heads(dK);
-      chunked<true, true>(d, dv, st);
-      heads(dV);
-    } else {
-      chunked<true, false>(d, dk, st);
-      chunked<true, false>(d, dv, st);
+    const size_t part = grouped ? (size_t)d.B * d.H * d.n * 64 * 4 : 0;  // a gradient's shares, fp32
+    Chunked a{};
+    a.log_decay = log_decay, a.lengths = lengths, a.seg = (float*)((char*)ws + 2 * part);
+    a.H = d.H, a.Hk = d.Hk, a.n = d.n, a.scale = scale;
+    Chunked b = a;
+    a.q = (const uint16_t*)dO, a.k = (const uint16_t*)V, a.v = (const uint16_t*)K;
+    a.k_shared = a.v_shared = true;
+    a.state = state, a.transposed = true, a.out = dQ;
+    b.q = (const uint16_t*)K, b.k = (const uint16_t*)Q, b.v = (const uint16_t*)dO, b.w = (const uint16_t*)V;
+    b.q_shared = b.w_shared = true;
+    b.state = dstate, b.state_out = dstate_out;
+    b.out = grouped ? ws : dV, b.out2 = grouped ? (char*)ws + part : dK;
+    const Split s = split_of(d, 2);
+    b.seg = a.seg + seg_bytes(d, s) / 4;
+    set_split(a, s);
+    set_split(b, s);
+    segment_states(d, a, b, 2, st);
+    {
+      TimedLaunch tl("lin_backward", st);
+      const int half = d.B * d.H * s.P;
+      const dim3 wgs((unsigned)(2 * half));
+      if (grouped)
+        hipLaunchKernelGGL(k_lin_backward<true>, wgs, dim3(512), 0, st, a, b, half);
+      else
+        hipLaunchKernelGGL(k_lin_backward<false>, wgs, dim3(512), 0, st, a, b, half);
     }
+    heads(b.out, dV);
+    heads(b.out2, dK);
     return hipGetLastError();
   }
   walk(d, Walk{dO, V, K, false, true, true, log_decay, state, lengths, nullptr, dQ, d.H, d.Hk, d.n, scale, false, true,
                false}, st);
   walk(d, Walk{V, dO, Q, true, false, false, log_decay, dstate, lengths, nullptr, grouped ? ws : dK, d.H, d.Hk, d.n,
                scale, true, true, grouped}, st);
-  heads(dK);
+  heads(ws, dK);
   walk(d, Walk{K, Q, dO, true, false, false, log_decay, dstate, lengths, dstate_out, grouped ? ws : dV, d.H, d.Hk, d.n,
                scale, true, false, grouped}, st);
-  heads(dV);
+  heads(ws, dV);
   return hipGetLastError();
 }
 
