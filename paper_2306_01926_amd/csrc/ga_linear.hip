@@ -44,75 +44,6 @@ __device__ __forceinline__ int length_of(const int32_t* lengths, int64_t b, int 
   return lengths ? min(max(lengths[b], 0), n) : n;
 }
 
-// One wave per slice: lane c holds column c of the state.
-struct Walk {
-  const void *q, *k, *v;   // roles (see above), [B][H or Hk][n][64]
-  bool q_shared, k_shared, v_shared;  // the tensor has Hk heads
-  const float *log_decay, *state;
-  const int32_t* lengths;
-  float* state_out;
-  void* out;    // [B][H][n][64] in the storage type, or fp32
-  int H, Hk, n;
-  float scale;
-  bool reverse, transposed, out_f32;
-};
-
-template <class DT>
-__global__ __launch_bounds__(64) void k_lin_walk(Walk A) {
-  using T = typename DT::T;
-  __shared__ float qs[kStep][64], ks[kStep][64];
-  const int c = threadIdx.x, h = blockIdx.x % A.H;
-  const int64_t b = blockIdx.x / A.H, bh = blockIdx.x, bk = b * A.Hk + h / (A.H / A.Hk);
-  const int len = length_of(A.lengths, b, A.n);
-  const T* q = (const T*)A.q + (A.q_shared ? bk : bh) * A.n * 64;
-  const T* k = (const T*)A.k + (A.k_shared ? bk : bh) * A.n * 64;
-  const T* v = (const T*)A.v + (A.v_shared ? bk : bh) * A.n * 64;
-  const Decay l(A.log_decay[h]);
-  float S[64];
-#pragma unroll
-  for (int a = 0; a < 64; ++a)
-    S[a] = !A.state ? 0.f : A.state[bh * 4096 + (A.transposed ? c * 64 + a : a * 64 + c)];
-  auto put = [&](int64_t token, float o) {
-    const int64_t at = (bh * A.n + token) * 64 + c;
-    if (A.out_f32)
-      ((float*)A.out)[at] = o;
-    else if constexpr (DT::kBits == 16)
-      ((T*)A.out)[at] = (T)(pack_bf16x2(o, 0.f) & 0xffffu);
-    else
-      ((T*)A.out)[at] = o;
-  };
-  for (int t0 = 0; t0 < len; t0 += kStep) {
-    float vr[kStep];
-    __syncthreads();
-#pragma unroll
-    for (int u = 0; u < kStep; ++u) {
-      const int t = min(t0 + u, len - 1);
-      const int64_t at = (int64_t)(A.reverse ? len - 1 - t : t) * 64 + c;
-      qs[u][c] = DT::load(q, at);
-      ks[u][c] = DT::load(k, at);
-      vr[u] = DT::load(v, at);
-    }
-    __syncthreads();
-#pragma unroll
-    for (int u = 0; u < kStep; ++u) {
-      if (t0 + u >= len) break;
-      float o = 0.f;
-#pragma unroll
-      for (int a = 0; a < 64; ++a) {
-        S[a] = A.reverse ? fmaf(ks[u][a] * A.scale, vr[u], S[a]) : fmaf(ks[u][a], vr[u], l(S[a]));
-        o = fmaf(qs[u][a], S[a], o);
-        if (A.reverse) S[a] = l(S[a]);
-      }
-      put(A.reverse ? len - 1 - (t0 + u) : t0 + u, A.reverse ? o : o * A.scale);
-    }
-  }
-  for (int t = len; t < A.n; ++t) put(t, 0.f);  // behind the sequence's end
-  if (A.state_out) {
-#pragma unroll
-    for (int a = 0; a < 64; ++a) A.state_out[bh * 4096 + a * 64 + c] = S[a];
-  }
-}
-
 // One token per sequence: 256 threads per slice, thread (r, g) holds rows
 // r + 16 u of the state at columns 4 g .. 4 g + 3.  Bound by the state, 16 KB
 // read and 16 KB written per slice; everything is fp32.
@@ -916,9 +847,16 @@ __global__ __launch_bounds__(512, 2) void k_lin_backward(Chunked F, Chunked B, i
 // Local states of the segments to the states before them, in place:
 // s_0 = the initial state, s_{p+1} = l^(tokens of p) s_p + local_p.
 // grid (slices 16, directions).
-__global__ __launch_bounds__(256) void k_lin_scan(Chunked F, Chunked B) {
-  const Chunked& A = blockIdx.y == 0 ? F : B;
-  if (!A.scanned) return;
+struct Scan {
+  float* seg;
+  const float *state, *log_decay;
+  const int32_t* lengths;
+  int H, n, P, tokens;  // tokens per segment
+  bool transposed, wanted;
+};
+__global__ __launch_bounds__(256) void k_lin_scan(Scan F, Scan B) {
+  const Scan& A = blockIdx.y == 0 ? F : B;
+  if (!A.wanted) return;
   const int64_t bh = blockIdx.x >> 4;
   const int e = (blockIdx.x & 15) * 256 + threadIdx.x;
   const float g = decay_log2(A.log_decay[bh % A.H]);
@@ -933,19 +871,208 @@ __global__ __launch_bounds__(256) void k_lin_scan(Chunked F, Chunked B) {
     for (int u = 0; u < 8; ++u) {
       if (p0 + u >= A.P) break;
       at[(int64_t)(p0 + u) * 4096] = s;
-      const int64_t tokens = min(max((int64_t)len - (int64_t)(p0 + u) * A.cps * kC, (int64_t)0), (int64_t)A.cps * kC);
+      const int64_t tokens = min(max((int64_t)len - (int64_t)(p0 + u) * A.tokens, (int64_t)0), (int64_t)A.tokens);
       s = fmaf(decay_pow(g, (float)tokens), s, local[u]);
     }
   }
 }
 
-void walk(const LinearDims& d, const Walk& w, hipStream_t st) {
-  TimedLaunch tl("lin_walk", st);
-  const dim3 grid((unsigned)(d.B * d.H));
-  if (d.dtype == 1)
-    hipLaunchKernelGGL(k_lin_walk<BF16>, grid, dim3(64), 0, st, w);
+// ---------------------------------------------------------------- fp32, by chunks
+//
+// The same by chunks of 32 tokens with the fp32 matrix instructions (32x32x2):
+// one operand value per lane and step, so the registers that hold a result are
+// an operand of the next product in any of the roles that the walk needs.  With
+// (r, hf) the lane and j(x) = 8 (x / 4) + 4 hf + x % 4 for x = 0..15:
+//   lane r holds K[r][j(x)], Q[r][j(x)] (features j(x) and 32 + j(x)),
+//   V[j(x)][r], K[j(x)][r] (tokens j(x)), S[j(x)][r] (features of k),
+//   scores^T[j(x)][r], O^T[j(x)][r].
+// Only the decayed keys, needed by column, pass through LDS.  A wave walks a
+// segment for one half of the value features without a barrier; a workgroup is
+// the halves of two segments, so that its waves take a SIMD each.
+// Bound by the matrix instructions' rate, 112 of 64 cycles per chunk and half:
+// the products are a quarter of the plain quadratic form's at 64 tokens, and
+// smaller chunks would add more to the state's products than they save.  Rows of
+// a later chunk are requested where the registers of this one's become free,
+// hundreds of cycles before their use.
+constexpr int kC32 = 32;
+
+struct Walk32 {
+  const float *q, *k, *v;             // roles (see the head of the file)
+  bool q_shared, k_shared, v_shared;  // the tensor has Hk heads
+  const float *log_decay, *state;
+  const int32_t* lengths;
+  float *seg, *state_out, *out;  // seg: [B H][P][64][64], local states or (outputs) the states before each segment
+  int H, Hk, n, P, tokens;       // segments per slice, tokens per segment (a multiple of 32)
+  float scale;
+  bool transposed;  // the state and seg are S^T in this walk's roles
+};
+
+__device__ __forceinline__ f32x16 mfma1(float a, float b, const f32x16& c) {
+  return __builtin_amdgcn_mfma_f32_32x32x2f32(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ float buf_load1(Buffer b, int off) {
+  return __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(b, off, 0, 0));
+}
+
+constexpr int kRow32 = 68;  // LDS row stride (floats): 16 rows' writes of 16 bytes meet all banks
+constexpr int kLds32 = kC32 * kRow32;
+
+// Segments 2 block and 2 block + 1 of `items` in all (STATES: without each slice's last).
+template <bool REV, bool STATES>
+__device__ __forceinline__ void walk32(const Walk32& A, int block, int items, float (*lds)[kLds32]) {
+  const int nseg = STATES ? A.P - 1 : A.P;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), item = 2 * block + (wave >> 1);
+  if (item >= items) return;  // (no barriers)
+  const int64_t bh = item / nseg;
+  const int p = (int)(item - bh * nseg), h = (int)(bh % A.H);
+  const int64_t b = bh / A.H, bk = b * A.Hk + h / (A.H / A.Hk);
+  const int len = __builtin_amdgcn_readfirstlane(length_of(A.lengths, b, A.n));
+  const int lane = threadIdx.x & 63, r = lane & 31, hf = lane >> 5;
+  const int ch = wave & 1;
+  float* kt = lds[wave];  // the decayed keys, a token a row
+  const float* q = A.q + (A.q_shared ? bk : bh) * A.n * 64;
+  const float* k = A.k + (A.k_shared ? bk : bh) * A.n * 64;
+  const float* v = A.v + (A.v_shared ? bk : bh) * A.n * 64 + 32 * ch;
+  float* out = A.out + bh * A.n * 64 + 32 * ch;
+  const float g = decay_log2(A.log_decay[h]);
+  const float ks = REV ? A.scale : 1.f;
+  const int64_t t0 = (int64_t)p * A.tokens, t1 = min(t0 + A.tokens, (int64_t)len);
+  auto jx = [&](int x) __attribute__((always_inline)) { return 8 * (x / 4) + 4 * hf + x % 4; };
+
+  // Rows of the chunk at walk position t.  Their buffer starts with the first of
+  // them in memory; rows behind the end are outside of it (v and out start 32 ch
+  // features into a row, so theirs ends as much behind the last one, where no
+  // lane reaches).
+  auto count = [&](int64_t t) __attribute__((always_inline)) { return (int)min(max(t1 - t, (int64_t)0), (int64_t)kC32); };
+  auto rows = [&](const float* base, int64_t t, int nr) __attribute__((always_inline)) {
+    return buffer(base + (REV ? (int64_t)len - t - nr : t) * 64, nr * 256);
+  };
+  auto place = [&](int x, int nr) __attribute__((always_inline)) { return REV ? nr - 1 - x : x; };
+
+  float qa[32], ka[32], vc[16];
+  auto load_row = [&](const float* base, int64_t t, float(&x)[32]) __attribute__((always_inline)) {
+    const int nr = count(t), off = place(r, nr) * 256 + 16 * hf;
+    const Buffer bf = rows(base, t, nr);
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {  // features 8 u + 4 hf + 0..3
+      const u32x4 y = buf_load(bf, off + 32 * u);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[4 * u + e] = __uint_as_float(y[e]);
+    }
+  };
+  auto load_values = [&](int64_t t) __attribute__((always_inline)) {
+    const int nr = count(t);
+    const Buffer bv = rows(v, t, nr);
+#pragma unroll
+    for (int x = 0; x < 16; ++x) vc[x] = buf_load1(bv, place(jx(x), nr) * 256 + 4 * r);
+  };
+  auto put_keys = [&](int nr) __attribute__((always_inline)) {
+    const float w = ks * decay_pow(g, (float)(max(nr - 1 - r, 0) + REV));  // (rows behind the end are zeros)
+#pragma unroll
+    for (int u = 0; u < 8; ++u)
+      *(float4*)(kt + r * kRow32 + 8 * u + 4 * hf) =
+          make_float4(w * ka[4 * u], w * ka[4 * u + 1], w * ka[4 * u + 2], w * ka[4 * u + 3]);
+  };
+
+  f32x16 S[2] = {zero16(), zero16()};  // S[32 e + j(x)][32 ch + r]
+  if (!STATES) {
+    const float* s0 = A.P > 1 ? A.seg + (bh * A.P + p) * 4096 : (A.state ? A.state + bh * 4096 : nullptr);
+    if (s0) {
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+#pragma unroll
+        for (int x = 0; x < 16; ++x) {
+          const int a = 32 * e + jx(x), c = 32 * ch + r;
+          S[e][x] = s0[A.transposed ? c * 64 + a : a * 64 + c];
+        }
+    }
+  }
+  float wd[16];
+#pragma unroll
+  for (int x = 0; x < 16; ++x) wd[x] = r >= jx(x) ? A.scale * decay_pow(g, (float)(r - jx(x))) : 0.f;
+  const float wi = (REV ? 1.f : A.scale) * decay_pow(g, (float)(r + 1 - REV));
+
+  if (t0 < t1) {
+    load_row(k, t0, ka);
+    if (!STATES) load_row(q, t0, qa);
+    load_values(t0);
+  }
+  for (int64_t t = t0; t < t1; t += kC32) {
+    const int nr = count(t);
+    f32x16 P = zero16(), oi = zero16(), o = zero16();
+    if (!STATES) {
+#pragma unroll
+      for (int x = 0; x < 32; ++x) P = mfma1(ka[x], qa[x], P);
+    }
+    put_keys(nr);
+    load_row(k, t + kC32, ka);
+    __builtin_amdgcn_sched_barrier(0);  // (or the compiler requests everything at the end)
+    if (!STATES) {
+#pragma unroll
+      for (int x = 0; x < 32; ++x) oi = mfma1(S[x / 16][x % 16], qa[x], oi);
+      load_row(q, t + kC32, qa);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int x = 0; x < 16; ++x) o = mfma1(vc[x], P[x] * wd[x], o);
+      const Buffer bo = rows(out, t, nr);
+      const int row = place(r, nr) * 256 + 16 * hf;
+#pragma unroll
+      for (int x = 0; x < 16; x += 4) {
+        u32x4 y;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] = __float_as_uint(fmaf(wi, oi[x + e], o[x + e]));
+        buf_store(bo, row + 8 * x, y);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    const float w = decay_pow(g, (float)nr);
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+#pragma unroll
+      for (int x = 0; x < 16; ++x) S[e][x] *= w;
+#pragma unroll
+    for (int x = 0; x < 16; ++x)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) S[e] = mfma1(kt[jx(x) * kRow32 + 32 * e + r], vc[x], S[e]);
+    load_values(t + kC32);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  float* so = STATES ? A.seg + (bh * A.P + p) * 4096
+                     : (p == A.P - 1 && A.state_out ? A.state_out + bh * 4096 : nullptr);
+  if (so) {
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+#pragma unroll
+      for (int x = 0; x < 16; ++x) so[(32 * e + jx(x)) * 64 + 32 * ch + r] = S[e][x];
+  }
+  if (!STATES) {  // rows behind the sequence's end
+    const int64_t z1 = p == A.P - 1 ? (int64_t)A.n : min((int64_t)A.n, t0 + A.tokens);
+    for (int64_t t = max((int64_t)len, t0) + (lane >> 3); t < z1; t += 8)
+      *(float4*)(out + t * 64 + 4 * (lane & 7)) = make_float4(0.f, 0.f, 0.f, 0.f);
+  }
+}
+
+// grid (segments but each slice's last / 2, directions): the local states of forward and backward walks.
+__global__ __launch_bounds__(256, 1) void k_lin_states_f32(Walk32 F, Walk32 B, int items) {
+  __shared__ __attribute__((aligned(16))) float lds[4][kLds32];
+  if (blockIdx.y == 0)
+    walk32<false, true>(F, blockIdx.x, items, lds);
   else
-    hipLaunchKernelGGL(k_lin_walk<F32>, grid, dim3(64), 0, st, w);
+    walk32<true, true>(B, blockIdx.x, items, lds);
+}
+// grid segments / 2.
+__global__ __launch_bounds__(256, 1) void k_lin_forward_f32(Walk32 A, int items) {
+  __shared__ __attribute__((aligned(16))) float lds[4][kLds32];
+  walk32<false, false>(A, blockIdx.x, items, lds);
+}
+// grid (segments / 2, walks): dQ, dK, dV from walk `from` on.
+__global__ __launch_bounds__(256, 1) void k_lin_backward_f32(Walk32 Q, Walk32 K, Walk32 V, int from, int items) {
+  __shared__ __attribute__((aligned(16))) float lds[4][kLds32];
+  const int walk = from + blockIdx.y;
+  if (walk == 0)
+    walk32<false, false>(Q, blockIdx.x, items, lds);
+  else
+    walk32<true, false>(walk == 1 ? K : V, blockIdx.x, items, lds);
 }
 
 // Segments per slice and chunks per segment.
@@ -986,13 +1113,53 @@ void segment_states(const LinearDims& d, const Chunked& f, const Chunked& b, uns
   }
   if (f.scanned || b.scanned) {
     TimedLaunch tl("lin_scan", st);
-    hipLaunchKernelGGL(k_lin_scan, dim3(slices * 16, directions), dim3(256), 0, st, f, b);
+    auto scan = [](const Chunked& c) {
+      return Scan{c.seg, c.state, c.log_decay, c.lengths, c.H, c.n, c.P, c.cps * kC, c.transposed, c.scanned};
+    };
+    hipLaunchKernelGGL(k_lin_scan, dim3(slices * 16, directions), dim3(256), 0, st, scan(f), scan(b));
   }
+}
+
+// fp32: a slice's two halves are a wave each, and one wave keeps a SIMD's
+// matrix unit busy (B H = 128, n = 4000: 195 us with one a SIMD, 206 with two,
+// 350 with half).  Two chunks of 64 at least to a segment.
+Split split32_of(const LinearDims& d, int walks) {
+  const int chunks = (d.n + kC - 1) / kC;
+  const int64_t all = (int64_t)d.B * d.H * walks * 2;
+  int64_t P = all >= 768 ? 1 : 1024 / all;
+  if (P > chunks / 2) P = chunks / 2;
+  if (P < 1) P = 1;
+  const int cps = (int)((chunks + P - 1) / P);
+  return Split{(chunks + cps - 1) / cps, cps};
+}
+
+Walk32 walk32_of(const LinearDims& d, Split s, const float* log_decay, const int32_t* lengths, float scale) {
+  Walk32 a{};
+  a.log_decay = log_decay, a.lengths = lengths, a.scale = scale;
+  a.H = d.H, a.Hk = d.Hk, a.n = d.n, a.P = s.P, a.tokens = s.cps * kC;
+  return a;
+}
+
+void segment_states32(const LinearDims& d, const Walk32& f, const Walk32& b, unsigned directions, hipStream_t st) {
+  if (f.P < 2) return;
+  const unsigned slices = (unsigned)(d.B * d.H);
+  {
+    TimedLaunch tl("lin_states", st);
+    const int items = (int)slices * (f.P - 1);
+    hipLaunchKernelGGL(k_lin_states_f32, dim3((items + 1) / 2, directions), dim3(256), 0, st, f, b, items);
+  }
+  auto scan = [](const Walk32& c) {
+    return Scan{c.seg, c.state, c.log_decay, c.lengths, c.H, c.n, c.P, c.tokens, false, true};
+  };
+  TimedLaunch tl("lin_scan", st);
+  hipLaunchKernelGGL(k_lin_scan, dim3(slices * 16, directions), dim3(256), 0, st, scan(f), scan(b));
 }
 
 }  // namespace
 
-size_t linear_workspace(const LinearDims& d) { return d.dtype == 1 ? seg_bytes(d, split_of(d, 1)) : 0; }
+size_t linear_workspace(const LinearDims& d) {
+  return seg_bytes(d, d.dtype == 1 ? split_of(d, 1) : split32_of(d, 1));
+}
 
 hipError_t launch_linear(const LinearDims& d, const void* Q, const void* K, const void* V, const float* log_decay,
                          const int32_t* lengths, const float* state, float scale, void* O, float* state_out, void* ws,
@@ -1010,20 +1177,28 @@ hipError_t launch_linear(const LinearDims& d, const void* Q, const void* K, cons
     hipLaunchKernelGGL(k_lin_forward, dim3((unsigned)(d.B * d.H * a.P)), dim3(512), 0, st, a);
     return hipGetLastError();
   }
-  walk(d, Walk{Q, K, V, false, true, true, log_decay, state, lengths, state_out, O, d.H, d.Hk, d.n, scale, false,
-               false, false}, st);
+  Walk32 a = walk32_of(d, split32_of(d, 1), log_decay, lengths, scale);
+  a.q = (const float*)Q, a.k = (const float*)K, a.v = (const float*)V;
+  a.k_shared = a.v_shared = true;
+  a.state = state, a.seg = (float*)ws, a.state_out = state_out, a.out = (float*)O;
+  segment_states32(d, a, Walk32{}, 1, st);
+  TimedLaunch tl("lin_forward", st);
+  const int items = d.B * d.H * a.P;
+  hipLaunchKernelGGL(k_lin_forward_f32, dim3((items + 1) / 2), dim3(256), 0, st, a, items);
   return hipGetLastError();
 }
 
 size_t linear_grad_workspace(const LinearDims& d) {
-  const size_t part = d.H == d.Hk ? 0 : (size_t)d.B * d.H * d.n * 64 * 4;  // a query head's share of dK or dV
-  return d.dtype == 1 ? 2 * part + 2 * seg_bytes(d, split_of(d, 2)) : part;
+  // a query head's shares of shared dK and dV, and the states before both walks' segments
+  const size_t part = d.H == d.Hk ? 0 : (size_t)d.B * d.H * d.n * 64 * 4;
+  return 2 * part + 2 * seg_bytes(d, d.dtype == 1 ? split_of(d, 2) : split32_of(d, 3));
 }
 
 hipError_t launch_linear_grad(const LinearDims& d, const void* Q, const void* K, const void* V, const void* dO,
                               const float* log_decay, const int32_t* lengths, const float* state, const float* dstate,
                               float scale, void* dQ, void* dK, void* dV, float* dstate_out, void* ws, hipStream_t st) {
   const bool grouped = d.H != d.Hk;
+  const size_t part = grouped ? (size_t)d.B * d.H * d.n * 64 * 4 : 0;
   const int64_t row4 = (int64_t)d.n * 16, total4 = (int64_t)d.B * d.Hk * row4;
   const unsigned grid = (unsigned)((total4 + 255) / 256 < 8192 ? (total4 + 255) / 256 : 8192);
   auto heads = [&](const void* part, void* out) {
@@ -1037,7 +1212,6 @@ hipError_t launch_linear_grad(const LinearDims& d, const void* Q, const void* K,
                          (float*)out);
   };
   if (d.dtype == 1) {
-    const size_t part = grouped ? (size_t)d.B * d.H * d.n * 64 * 4 : 0;  // a gradient's shares, fp32
     Chunked a{};
     a.log_decay = log_decay, a.lengths = lengths, a.seg = (float*)((char*)ws + 2 * part);
     a.H = d.H, a.Hk = d.Hk, a.n = d.n, a.scale = scale;
@@ -1067,14 +1241,30 @@ hipError_t launch_linear_grad(const LinearDims& d, const void* Q, const void* K,
     heads(b.out2, dK);
     return hipGetLastError();
   }
-  walk(d, Walk{dO, V, K, false, true, true, log_decay, state, lengths, nullptr, dQ, d.H, d.Hk, d.n, scale, false, true,
-               false}, st);
-  walk(d, Walk{V, dO, Q, true, false, false, log_decay, dstate, lengths, nullptr, grouped ? ws : dK, d.H, d.Hk, d.n,
-               scale, true, true, grouped}, st);
-  heads(ws, dK);
-  walk(d, Walk{K, Q, dO, true, false, false, log_decay, dstate, lengths, dstate_out, grouped ? ws : dV, d.H, d.Hk, d.n,
-               scale, true, false, grouped}, st);
-  heads(ws, dV);
+  const Split s = split32_of(d, 3);
+  // the states of both directions, S[k feature][v feature] and R[q feature][dO feature]
+  Walk32 f = walk32_of(d, s, log_decay, lengths, scale), r = f;
+  f.k = (const float*)K, f.v = (const float*)V, f.k_shared = f.v_shared = true;
+  f.q = (const float*)Q, r.q = (const float*)K;
+  r.k = (const float*)Q, r.v = (const float*)dO, r.q_shared = true;
+  f.seg = (float*)((char*)ws + 2 * part), r.seg = f.seg + seg_bytes(d, s) / 4;
+  f.state = state, r.state = dstate;
+  segment_states32(d, f, r, 2, st);
+  Walk32 dq = f, dv = r, dk = r;
+  dq.q = (const float*)dO, dq.k = (const float*)V, dq.v = (const float*)K, dq.transposed = true, dq.out = (float*)dQ;
+  dv.out = grouped ? (float*)ws : (float*)dV, dv.state_out = dstate_out;
+  dk.q = (const float*)V, dk.k = (const float*)dO, dk.v = (const float*)Q, dk.transposed = true;
+  dk.out = grouped ? (float*)((char*)ws + part) : (float*)dK;
+  {
+    TimedLaunch tl("lin_backward", st);
+    const int items = d.B * d.H * s.P, wgs = (items + 1) / 2;
+    // a final state's gradient that is updated in place by dV's walk is read by dK's first
+    const bool apart = s.P == 1 && dstate && dstate == dstate_out;
+    hipLaunchKernelGGL(k_lin_backward_f32, dim3(wgs, apart ? 2 : 3), dim3(256), 0, st, dq, dk, dv, 0, items);
+    if (apart) hipLaunchKernelGGL(k_lin_backward_f32, dim3(wgs, 1), dim3(256), 0, st, dq, dk, dv, 2, items);
+  }
+  heads(dv.out, dV);
+  heads(dk.out, dK);
   return hipGetLastError();
 }
 
