@@ -38,29 +38,41 @@ namespace {
 
 constexpr int kE = 8;  // features per thread
 
-// Eight features of one row from column c (beyond W: zeros).  VEC: W is a
+// Eight features of one row from column c (beyond W: zeros), as they come from
+// memory: requested a row ahead, converted where they are used.  VEC: W is a
 // multiple of eight, so every group of eight is whole and 16-byte aligned.
 template <class DT, bool VEC>
-__device__ __forceinline__ void load8(const typename DT::T* p, int c, int W, float (&v)[kE]) {
-  if constexpr (VEC) {
-    if (c >= W) {
+struct Eight {
+  static constexpr int kWords = VEC ? (DT::kBits == 16 ? 1 : 2) : 0;
+  u32x4 w[kWords ? kWords : 1];
+  typename DT::T s[kWords ? 1 : kE];
+
+  __device__ __forceinline__ void load(const typename DT::T* p, int c, int W) {
+    if constexpr (VEC) {
 #pragma unroll
-      for (int e = 0; e < kE; ++e) v[e] = 0.f;
-    } else if constexpr (DT::kBits == 16) {
-      const u32x4 w = *(const u32x4*)(p + c);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        v[2 * e] = bf16_to_f32(w[e] & 0xffffu);
-        v[2 * e + 1] = bf16_to_f32(w[e] >> 16);
-      }
+      for (int i = 0; i < kWords; ++i) w[i] = c < W ? *(const u32x4*)(p + c + 4 * i) : u32x4{0u, 0u, 0u, 0u};
     } else {
-      const float4 a = *(const float4*)(p + c), b = *(const float4*)(p + c + 4);
-      v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
-    }
-  } else {
 #pragma unroll
-    for (int e = 0; e < kE; ++e) v[e] = c + e < W ? DT::load(p, c + e) : 0.f;
+      for (int e = 0; e < kE; ++e) s[e] = c + e < W ? p[c + e] : (typename DT::T)0;
+    }
   }
+  __device__ __forceinline__ void get(float (&v)[kE]) const {
+#pragma unroll
+    for (int e = 0; e < kE; ++e) {
+      if constexpr (!VEC)
+        v[e] = DT::load(s, e);
+      else if constexpr (DT::kBits == 16)
+        v[e] = __uint_as_float(e & 1 ? w[0][e / 2] & 0xffff0000u : w[0][e / 2] << 16);
+      else
+        v[e] = __uint_as_float(w[e / 4][e % 4]);
+    }
+  }
+};
+template <class DT, bool VEC>
+__device__ __forceinline__ void load8(const typename DT::T* p, int c, int W, float (&v)[kE]) {
+  Eight<DT, VEC> x;
+  x.load(p, c, W);
+  x.get(v);
 }
 
 // The outputs are rounded once, to nearest even (bf16), here.
@@ -89,6 +101,26 @@ __device__ __forceinline__ void store8(typename DT::T* p, int c, int W, const fl
   }
 }
 
+// The sum over groups of min(TPR, 64) lanes, in each of them, by lane exchanges
+// of the VALU (an exchange through LDS takes ten times as long, and a row waits
+// for up to eight sums one after another).
+template <int TPR>
+__device__ __forceinline__ float lanes_sum(float x) {
+  x += __int_as_float(dpp<kXor1>(__float_as_int(x)));
+  x += __int_as_float(dpp<kXor2>(__float_as_int(x)));
+  x += __int_as_float(dpp<kHalfMirror>(__float_as_int(x)));
+  if constexpr (TPR >= 16) x += __int_as_float(dpp<kMirror>(__float_as_int(x)));
+  if constexpr (TPR >= 32) {
+    const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = __uint_as_float(p[0]) + __uint_as_float(p[1]);
+  }
+  if constexpr (TPR >= 64) {
+    const u32x2 q = halves(__float_as_uint(x));
+    x = __uint_as_float(q[0]) + __uint_as_float(q[1]);
+  }
+  return x;
+}
+
 // Sums of two values over the TPR threads of a team, in every thread of it.
 // Teams of more than a wave exchange through red[16], one entry per wave.
 // The calls inside one row's work have a red each, and rows alternate between
@@ -97,11 +129,8 @@ __device__ __forceinline__ void store8(typename DT::T* p, int c, int W, const fl
 // it.
 template <int TPR>
 __device__ __forceinline__ float2 team_sum(float a, float b, float2* red) {
-#pragma unroll
-  for (int m = 1; m < (TPR < 64 ? TPR : 64); m <<= 1) {
-    a += __shfl_xor(a, m);
-    b += __shfl_xor(b, m);
-  }
+  a = lanes_sum<TPR>(a);
+  b = lanes_sum<TPR>(b);
   if constexpr (TPR > 64) {
     constexpr int kW = TPR / 64;  // waves per team
     const int wave = threadIdx.x >> 6, first = wave / kW * kW;
@@ -135,7 +164,7 @@ __device__ __forceinline__ float normalise(float (&z)[kE], int c, int W, float i
   float q = 0.f;
 #pragma unroll
   for (int e = 0; e < kE; ++e) q = fmaf(z[e], z[e], q);
-  const float r = 1.0f / sqrtf(team_sum<TPR>(q, 0.f, red[1]).x * invW + eps);
+  const float r = rsqrtf(team_sum<TPR>(q, 0.f, red[1]).x * invW + eps);
 #pragma unroll
   for (int e = 0; e < kE; ++e) z[e] *= r;
   return r;
@@ -181,16 +210,27 @@ __global__ __launch_bounds__(wg_threads(TPR)) void k_norm(NormArgs<DT> A, typena
   if (Ho) load8<DT, VEC>(A.pre_w, c, W, qw);
   if (Ho && A.pre_b) load8<DT, VEC>(A.pre_b, c, W, qb);
   int parity = 0;
+  const int64_t step = (int64_t)gridDim.x * kTeams;
+  Eight<DT, VEC> nx, nf, ng;  // the next row
+  auto request = [&](int64_t row0) __attribute__((always_inline)) {
+    const int64_t row = min(row0 + team, A.rows - 1);
+    nx.load(A.X + row * W, c, W);
+    if (A.F) nf.load(A.F + row * W, c, W);
+    if (A.gate_batches > 1)
+      ng.load(A.gate + (A.rows <= INT32_MAX ? (int64_t)((uint32_t)row / (uint32_t)A.n) : row / A.n) * W, c, W);
+  };
+  request((int64_t)blockIdx.x * kTeams);
   // every team makes the same number of turns (barriers inside)
-  for (int64_t row0 = (int64_t)blockIdx.x * kTeams; row0 < A.rows; row0 += (int64_t)gridDim.x * kTeams) {
+  for (int64_t row0 = (int64_t)blockIdx.x * kTeams; row0 < A.rows; row0 += step) {
     float2(*red)[16] = reds[parity];
     parity ^= 1;
     const bool live = row0 + team < A.rows;
-    const int64_t row = live ? row0 + team : A.rows - 1;
+    const int64_t row = min(row0 + team, A.rows - 1);
     float y[kE], u[kE];
-    load8<DT, VEC>(A.X + row * W, c, W, y);
-    if (A.F) load8<DT, VEC>(A.F + row * W, c, W, u);
-    if (A.gate_batches > 1) load8<DT, VEC>(A.gate + row / A.n * W, c, W, gt);
+    nx.get(y);
+    if (A.F) nf.get(u);
+    if (A.gate_batches > 1) ng.get(gt);
+    request(row0 + step);
 #pragma unroll
     for (int e = 0; e < kE; ++e) y[e] *= A.a;
     if (A.F) {
@@ -261,21 +301,31 @@ __global__ __launch_bounds__(wg_threads(TPR)) void k_norm_grad(NormArgs<DT> A, c
 #pragma unroll
     for (int e = 0; e < kE; ++e) sg[e] = 0.f;
     if (A.gate_batches) load8<DT, VEC>(A.gate + (A.gate_batches > 1 ? (int64_t)grp * W : 0), c, W, gt);
+    Eight<DT, VEC> nx, nf, ny, nh;  // the next row
+    auto request = [&](int64_t r0) __attribute__((always_inline)) {
+      const int64_t at = (grp * P.group_rows + min(r0 + team, P.group_rows - 1)) * W;
+      nx.load(A.X + at, c, W);
+      if (A.F) nf.load(A.F + at, c, W);
+      if (dY) ny.load(dY + at, c, W);
+      if (dH) nh.load(dH + at, c, W);
+    };
+    request((int64_t)share * kTeams);
     for (int64_t r0 = (int64_t)share * kTeams; r0 < P.group_rows; r0 += (int64_t)P.split * kTeams) {
       float2(*red)[16] = reds[parity];
       parity ^= 1;
       const bool live = r0 + team < P.group_rows;
       const int64_t row = grp * P.group_rows + (live ? r0 + team : P.group_rows - 1);
       float y[kE], u[kE], fn[kE], d[kE], dh[kE], rf = 0.f;
-      load8<DT, VEC>(A.X + row * W, c, W, y);
-      if (A.F) load8<DT, VEC>(A.F + row * W, c, W, fn);
+      nx.get(y);
+      if (A.F) nf.get(fn);
       if (dY) {
-        load8<DT, VEC>(dY + row * W, c, W, d);
+        ny.get(d);
       } else {
 #pragma unroll
         for (int e = 0; e < kE; ++e) d[e] = 0.f;
       }
-      if (dH) load8<DT, VEC>(dH + row * W, c, W, dh);
+      if (dH) nh.get(dh);
+      request(r0 + (int64_t)P.split * kTeams);
 #pragma unroll
       for (int e = 0; e < kE; ++e) y[e] *= A.a;
       if (A.F) {
