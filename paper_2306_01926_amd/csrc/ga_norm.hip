@@ -40,28 +40,39 @@ constexpr int kE = 8;  // features per thread
 
 // Eight features of one row from column c (beyond W: zeros), as they come from
 // memory: requested a row ahead, converted where they are used.  VEC: W is a
-// multiple of eight, so every group of eight is whole and 16-byte aligned.
+// multiple of eight, so every group of eight is whole and 16-byte aligned; else
+// groups are read and written in one piece at any alignment (global memory
+// allows it) and a row's last, incomplete one by single features.
+struct __attribute__((packed, aligned(2))) Piece {
+  u32x4 w;
+};
 template <class DT, bool VEC>
 struct Eight {
-  static constexpr int kWords = VEC ? (DT::kBits == 16 ? 1 : 2) : 0;
-  u32x4 w[kWords ? kWords : 1];
-  typename DT::T s[kWords ? 1 : kE];
+  using T = typename DT::T;
+  static constexpr int kWords = DT::kBits == 16 ? 1 : 2, kPer = kE / kWords;  // 16-byte words, features in one
+  u32x4 w[kWords];
 
-  __device__ __forceinline__ void load(const typename DT::T* p, int c, int W) {
-    if constexpr (VEC) {
+  __device__ __forceinline__ void load(const T* p, int c, int W) {
 #pragma unroll
-      for (int i = 0; i < kWords; ++i) w[i] = c < W ? *(const u32x4*)(p + c + 4 * i) : u32x4{0u, 0u, 0u, 0u};
-    } else {
+    for (int i = 0; i < kWords; ++i) w[i] = u32x4{0u, 0u, 0u, 0u};
+    if (VEC ? c < W : c + kE <= W) {
 #pragma unroll
-      for (int e = 0; e < kE; ++e) s[e] = c + e < W ? p[c + e] : (typename DT::T)0;
+      for (int i = 0; i < kWords; ++i) w[i] = VEC ? *(const u32x4*)(p + c + kPer * i) : ((const Piece*)(p + c + kPer * i))->w;
+    } else if (!VEC) {
+#pragma unroll
+      for (int e = 0; e < kE; ++e) {
+        if (c + e >= W) continue;
+        if constexpr (DT::kBits == 16)
+          w[0][e / 2] |= (uint32_t)p[c + e] << (16 * (e & 1));
+        else
+          w[e / 4][e % 4] = __float_as_uint(p[c + e]);
+      }
     }
   }
   __device__ __forceinline__ void get(float (&v)[kE]) const {
 #pragma unroll
     for (int e = 0; e < kE; ++e) {
-      if constexpr (!VEC)
-        v[e] = DT::load(s, e);
-      else if constexpr (DT::kBits == 16)
+      if constexpr (DT::kBits == 16)
         v[e] = __uint_as_float(e & 1 ? w[0][e / 2] & 0xffff0000u : w[0][e / 2] << 16);
       else
         v[e] = __uint_as_float(w[e / 4][e % 4]);
@@ -78,23 +89,31 @@ __device__ __forceinline__ void load8(const typename DT::T* p, int c, int W, flo
 // The outputs are rounded once, to nearest even (bf16), here.
 template <class DT, bool VEC>
 __device__ __forceinline__ void store8(typename DT::T* p, int c, int W, const float (&v)[kE]) {
-  if constexpr (VEC) {
-    if (c >= W) return;
-    if constexpr (DT::kBits == 16) {
-      u32x4 w;
+  using E = Eight<DT, VEC>;
+  u32x4 w[E::kWords];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) w[e] = pack_bf16x2(v[2 * e], v[2 * e + 1]);
-      *(u32x4*)(p + c) = w;
+  for (int e = 0; e < kE; e += 2) {
+    if constexpr (DT::kBits == 16) {
+      w[0][e / 2] = pack_bf16x2(v[e], v[e + 1]);
     } else {
-      *(float4*)(p + c) = make_float4(v[0], v[1], v[2], v[3]);
-      *(float4*)(p + c + 4) = make_float4(v[4], v[5], v[6], v[7]);
+      w[e / 4][e % 4] = __float_as_uint(v[e]);
+      w[e / 4][e % 4 + 1] = __float_as_uint(v[e + 1]);
     }
-  } else {
+  }
+  if (VEC ? c < W : c + kE <= W) {
+#pragma unroll
+    for (int i = 0; i < E::kWords; ++i) {
+      if (VEC)
+        *(u32x4*)(p + c + E::kPer * i) = w[i];
+      else
+        ((Piece*)(p + c + E::kPer * i))->w = w[i];
+    }
+  } else if (!VEC) {
 #pragma unroll
     for (int e = 0; e < kE; ++e) {
       if (c + e >= W) continue;
       if constexpr (DT::kBits == 16)
-        p[c + e] = (uint16_t)(pack_bf16x2(v[e], 0.f) & 0xffffu);
+        p[c + e] = (uint16_t)(w[0][e / 2] >> (16 * (e & 1)));
       else
         p[c + e] = v[e];
     }
