@@ -40,9 +40,11 @@ constexpr int kE = 8;  // features per thread
 
 // Eight features of one row from column c (beyond W: zeros), as they come from
 // memory: requested a row ahead, converted where they are used.  VEC: W is a
-// multiple of eight, so every group of eight is whole and 16-byte aligned; else
+// multiple of eight, so every group of eight is whole and 16-byte aligned.  Else
 // groups are read and written in one piece at any alignment (global memory
-// allows it) and a row's last, incomplete one by single features.
+// allows it); a row's last, incomplete one is read with the features before it
+// and shifted where it is used (rows of fewer than eight: by single features),
+// and written by single features.
 struct __attribute__((packed, aligned(2))) Piece {
   u32x4 w;
 };
@@ -50,33 +52,77 @@ template <class DT, bool VEC>
 struct Eight {
   using T = typename DT::T;
   static constexpr int kWords = DT::kBits == 16 ? 1 : 2, kPer = kE / kWords;  // 16-byte words, features in one
-  u32x4 w[kWords];
+  uint32_t w[4 * kWords];
+  int behind;  // features read that lie before column c; kE: none is wanted
 
   __device__ __forceinline__ void load(const T* p, int c, int W) {
-#pragma unroll
-    for (int i = 0; i < kWords; ++i) w[i] = u32x4{0u, 0u, 0u, 0u};
-    if (VEC ? c < W : c + kE <= W) {
-#pragma unroll
-      for (int i = 0; i < kWords; ++i) w[i] = VEC ? *(const u32x4*)(p + c + kPer * i) : ((const Piece*)(p + c + kPer * i))->w;
-    } else if (!VEC) {
+    if (VEC) {
+      if (c < W) {
+        put(p + c);
+      } else {
+        zero();
+      }
+      return;
+    }
+    behind = min(max(c - (W - kE), 0), kE);
+    if (W >= kE) {
+      put(p + min(c, W - kE));
+    } else {
+      zero();
+      behind = 0;
 #pragma unroll
       for (int e = 0; e < kE; ++e) {
         if (c + e >= W) continue;
         if constexpr (DT::kBits == 16)
-          w[0][e / 2] |= (uint32_t)p[c + e] << (16 * (e & 1));
+          w[e / 2] |= (uint32_t)p[c + e] << (16 * (e & 1));
         else
-          w[e / 4][e % 4] = __float_as_uint(p[c + e]);
+          w[e] = __float_as_uint(p[c + e]);
       }
     }
   }
   __device__ __forceinline__ void get(float (&v)[kE]) const {
+    constexpr int kN = 4 * kWords;
+    uint32_t x[kN];
+#pragma unroll
+    for (int i = 0; i < kN; ++i) x[i] = w[i];
+    if constexpr (!VEC) {
+#pragma unroll
+      for (int s = kE; s >= 1; s /= 2) {  // by 8, 4, 2 and 1 features
+        const bool on = (behind & s) != 0;
+#pragma unroll
+        for (int i = 0; i < kN; ++i) {
+          if constexpr (DT::kBits == 16) {
+            const uint32_t hi = i + 1 < kN ? x[i + 1] : 0u;
+            const uint32_t y = s == 1 ? x[i] >> 16 | hi << 16 : (i + s / 2 < kN ? x[i + s / 2 < kN ? i + s / 2 : 0] : 0u);
+            x[i] = on ? y : x[i];
+          } else {
+            const uint32_t y = i + s < kN ? x[i + s < kN ? i + s : 0] : 0u;
+            x[i] = on ? y : x[i];
+          }
+        }
+      }
+    }
 #pragma unroll
     for (int e = 0; e < kE; ++e) {
       if constexpr (DT::kBits == 16)
-        v[e] = __uint_as_float(e & 1 ? w[0][e / 2] & 0xffff0000u : w[0][e / 2] << 16);
+        v[e] = __uint_as_float(e & 1 ? x[e / 2] & 0xffff0000u : x[e / 2] << 16);
       else
-        v[e] = __uint_as_float(w[e / 4][e % 4]);
+        v[e] = __uint_as_float(x[e]);
     }
+  }
+
+ private:
+  __device__ __forceinline__ void put(const T* p) {
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) {
+      const u32x4 y = VEC ? *(const u32x4*)(p + kPer * i) : ((const Piece*)(p + kPer * i))->w;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) w[4 * i + j] = y[j];
+    }
+  }
+  __device__ __forceinline__ void zero() {
+#pragma unroll
+    for (int i = 0; i < 4 * kWords; ++i) w[i] = 0u;
   }
 };
 template <class DT, bool VEC>
@@ -189,18 +235,8 @@ __device__ __forceinline__ float normalise(float (&z)[kE], int c, int W, float i
   return r;
 }
 
-// d -> P(d) in place (see the head of the file).
-template <int TPR>
-__device__ __forceinline__ void project(float (&d)[kE], const float (&zn)[kE], float r, int c, int W, float invW,
-                                        bool layer, float2* red) {
-  float s = 0.f, t = 0.f;
-#pragma unroll
-  for (int e = 0; e < kE; ++e) {
-    s = fmaf(d[e], zn[e], s);
-    t += d[e];
-  }
-  const float2 m = team_sum<TPR>(s, t, red);
-  const float mz = m.x * invW, md = layer ? m.y * invW : 0.f;
+// d -> P(d) in place (see the head of the file): mz = mean(d zn), md = mean d or 0.
+__device__ __forceinline__ void project(float (&d)[kE], const float (&zn)[kE], float r, float mz, float md, int c, int W) {
 #pragma unroll
   for (int e = 0; e < kE; ++e) d[e] = c + e < W ? r * (d[e] - fmaf(zn[e], mz, md)) : 0.f;
 }
@@ -295,20 +331,22 @@ __device__ __forceinline__ void team_store(const float (&v)[kE], float* buf, flo
   }
 }
 
-template <class DT, int TPR, bool VEC>
+// BIAS: the gradients of the norms' biases are asked for.
+template <class DT, int TPR, bool VEC, bool BIAS>
 __global__ __launch_bounds__(wg_threads(TPR)) void k_norm_grad(NormArgs<DT> A, const typename DT::T* __restrict__ dY,
                                                                const typename DT::T* __restrict__ dH,
                                                                typename DT::T* __restrict__ dX,
                                                                typename DT::T* __restrict__ dF, NormParts P) {
   constexpr int kT = wg_threads(TPR), kTeams = kT / TPR;
+  using Raw = Eight<DT, VEC>;
   __shared__ float2 reds[2][6][16];
   __shared__ float buf[kT * kE];
   const int team = threadIdx.x / TPR, c = (threadIdx.x % TPR) * kE, W = A.W;
-  float pw[kE], pb[kE], gt[kE], qw[kE];
-  if (A.post_w) load8<DT, VEC>(A.post_w, c, W, pw);
-  if (A.post_b) load8<DT, VEC>(A.post_b, c, W, pb);
-  if (dH) load8<DT, VEC>(A.pre_w, c, W, qw);
-  float spw[kE], spb[kE], sqw[kE], sqb[kE], sg[kE];
+  Raw pw, pb, gt, qw;  // (as stored: half the registers)
+  if (A.post_w) pw.load(A.post_w, c, W);
+  if (A.post_b) pb.load(A.post_b, c, W);
+  if (dH) qw.load(A.pre_w, c, W);
+  float spw[kE], sqw[kE], sg[kE], spb[kE], sqb[kE];
 #pragma unroll
   for (int e = 0; e < kE; ++e) spw[e] = spb[e] = sqw[e] = sqb[e] = 0.f;
 
@@ -319,8 +357,8 @@ __global__ __launch_bounds__(wg_threads(TPR)) void k_norm_grad(NormArgs<DT> A, c
     const int share = P.split > 1 ? blockIdx.x % P.split : 0;
 #pragma unroll
     for (int e = 0; e < kE; ++e) sg[e] = 0.f;
-    if (A.gate_batches) load8<DT, VEC>(A.gate + (A.gate_batches > 1 ? (int64_t)grp * W : 0), c, W, gt);
-    Eight<DT, VEC> nx, nf, ny, nh;  // the next row
+    if (A.gate_batches) gt.load(A.gate + (A.gate_batches > 1 ? (int64_t)grp * W : 0), c, W);
+    Raw nx, nf, ny, nh;  // the next row
     auto request = [&](int64_t r0) __attribute__((always_inline)) {
       const int64_t at = (grp * P.group_rows + min(r0 + team, P.group_rows - 1)) * W;
       nx.load(A.X + at, c, W);
@@ -332,9 +370,10 @@ __global__ __launch_bounds__(wg_threads(TPR)) void k_norm_grad(NormArgs<DT> A, c
     for (int64_t r0 = (int64_t)share * kTeams; r0 < P.group_rows; r0 += (int64_t)P.split * kTeams) {
       float2(*red)[16] = reds[parity];
       parity ^= 1;
-      const bool live = r0 + team < P.group_rows;
-      const int64_t row = grp * P.group_rows + (live ? r0 + team : P.group_rows - 1);
-      float y[kE], u[kE], fn[kE], d[kE], dh[kE], rf = 0.f;
+      // a team behind the last row works on it again, and its sums count nothing
+      const float live = r0 + team < P.group_rows ? 1.f : 0.f;
+      const int64_t row = grp * P.group_rows + min(r0 + team, P.group_rows - 1);
+      float y[kE], fn[kE], d[kE], dh[kE], w[kE], g[kE], rf = 0.f;
       nx.get(y);
       if (A.F) nf.get(fn);
       if (dY) {
@@ -347,57 +386,95 @@ __global__ __launch_bounds__(wg_threads(TPR)) void k_norm_grad(NormArgs<DT> A, c
       request(r0 + (int64_t)P.split * kTeams);
 #pragma unroll
       for (int e = 0; e < kE; ++e) y[e] *= A.a;
-      if (A.F) {
+      // u = w fn + c, formed where it is used
+      auto branch = [&](float(&u)[kE]) __attribute__((always_inline)) {
         if (A.post_w) {
-          rf = normalise<TPR>(fn, c, W, A.invW, A.layer, A.eps, red);
+          pw.get(u);
+          float s[kE];
+          if (A.post_b) pb.get(s);
 #pragma unroll
-          for (int e = 0; e < kE; ++e) u[e] = fmaf(fn[e], pw[e], A.post_b ? pb[e] : 0.f);
+          for (int e = 0; e < kE; ++e) u[e] = fmaf(fn[e], u[e], A.post_b ? s[e] : 0.f);
         } else {
 #pragma unroll
           for (int e = 0; e < kE; ++e) u[e] = fn[e];
         }
+      };
+      auto gates = [&]() __attribute__((always_inline)) {
+        if (A.gate_batches) gt.get(g);
 #pragma unroll
-        for (int e = 0; e < kE; ++e) y[e] = fmaf(A.gate_batches ? A.b * gt[e] : A.b, u[e], y[e]);
+        for (int e = 0; e < kE; ++e) g[e] = A.gate_batches ? A.b * g[e] : A.b;
+      };
+      if (A.F) {
+        if (A.post_w) rf = normalise<TPR>(fn, c, W, A.invW, A.layer, A.eps, red);
+        branch(w);
+        gates();
+#pragma unroll
+        for (int e = 0; e < kE; ++e) y[e] = fmaf(g[e], w[e], y[e]);
       }
       if (dH) {
-        const float rh = normalise<TPR>(y, c, W, A.invW, A.layer, A.eps, red + 2);
-        float dn[kE];
+        // the sums that the projection needs go with those of the norm
+        float sd = 0.f;
+        qw.get(w);
 #pragma unroll
         for (int e = 0; e < kE; ++e) {
-          if (live) {
-            sqw[e] = fmaf(dh[e], y[e], sqw[e]);
-            sqb[e] += dh[e];
-          }
-          dn[e] = dh[e] * qw[e];
-          if (c + e >= W) dn[e] = 0.f;
+          w[e] *= dh[e];  // (zeros beyond W)
+          sd += w[e];
         }
-        project<TPR>(dn, y, rh, c, W, A.invW, A.layer, red[4]);
+        float md = 0.f;
+        if (A.layer) {
+          float s = 0.f;
 #pragma unroll
-        for (int e = 0; e < kE; ++e) d[e] += dn[e];
+          for (int e = 0; e < kE; ++e) s += y[e];
+          const float2 m = team_sum<TPR>(s, sd, red[2]);
+          md = m.y * A.invW;
+#pragma unroll
+          for (int e = 0; e < kE; ++e) y[e] = c + e < W ? y[e] - m.x * A.invW : 0.f;
+        }
+        float q = 0.f, s = 0.f;
+#pragma unroll
+        for (int e = 0; e < kE; ++e) {
+          q = fmaf(y[e], y[e], q);
+          s = fmaf(w[e], y[e], s);
+        }
+        const float2 m = team_sum<TPR>(q, s, red[3]);
+        const float rh = rsqrtf(m.x * A.invW + A.eps);
+#pragma unroll
+        for (int e = 0; e < kE; ++e) {
+          y[e] *= rh;
+          dh[e] *= live;
+          sqw[e] = fmaf(dh[e], y[e], sqw[e]);
+          if (BIAS) sqb[e] += dh[e];
+        }
+        project(w, y, rh, rh * m.y * A.invW, md, c, W);
+#pragma unroll
+        for (int e = 0; e < kE; ++e) d[e] += w[e];
       }
       if (A.F) {
         float du[kE];
+        branch(w);
+        gates();
 #pragma unroll
         for (int e = 0; e < kE; ++e) {
-          const float bd = A.b * d[e];
-          if (live) sg[e] = fmaf(bd, u[e], sg[e]);
-          du[e] = A.gate_batches ? bd * gt[e] : bd;
+          sg[e] = fmaf(live * A.b * d[e], w[e], sg[e]);
+          du[e] = g[e] * d[e];
         }
         if (A.post_w) {
+          pw.get(w);
+          float s = 0.f, sd = 0.f;
 #pragma unroll
           for (int e = 0; e < kE; ++e) {
-            if (live) {
-              spw[e] = fmaf(du[e], fn[e], spw[e]);
-              spb[e] += du[e];
-            }
-            du[e] *= pw[e];
-            if (c + e >= W) du[e] = 0.f;
+            spw[e] = fmaf(live * du[e], fn[e], spw[e]);
+            if (BIAS) spb[e] = fmaf(live, du[e], spb[e]);
+            du[e] = c + e < W ? du[e] * w[e] : 0.f;
+            s = fmaf(du[e], fn[e], s);
+            sd += du[e];
           }
-          project<TPR>(du, fn, rf, c, W, A.invW, A.layer, red[5]);
+          const float2 m = team_sum<TPR>(s, sd, red[5]);
+          project(du, fn, rf, m.x * A.invW, A.layer ? m.y * A.invW : 0.f, c, W);
         }
-        if (dF && live) store8<DT, VEC>(dF + row * W, c, W, du);
+        if (dF && live != 0.f) store8<DT, VEC>(dF + row * W, c, W, du);
       }
-      if (dX && live) {
+      if (dX && live != 0.f) {
 #pragma unroll
         for (int e = 0; e < kE; ++e) d[e] *= A.a;
         store8<DT, VEC>(dX + row * W, c, W, d);
@@ -409,24 +486,24 @@ __global__ __launch_bounds__(wg_threads(TPR)) void k_norm_grad(NormArgs<DT> A, c
     float* dst = P.part + (int64_t)blockIdx.x * 4 * W;
     if (A.post_w) {
       team_store<TPR>(spw, buf, dst, W);
-      team_store<TPR>(spb, buf, dst + W, W);
+      if (BIAS) team_store<TPR>(spb, buf, dst + W, W);
     }
     if (dH) {
       team_store<TPR>(sqw, buf, dst + 2 * W, W);
-      team_store<TPR>(sqb, buf, dst + 3 * W, W);
+      if (BIAS) team_store<TPR>(sqb, buf, dst + 3 * W, W);
     }
   }
 }
 
 // out[g][col] = sum over parts p of src[(g parts + p) stride + col], in
-// ascending order within each of 16 interleaved shares.  grid (ceil(W / 16),
+// ascending order within each of 64 interleaved shares.  grid (ceil(W / 16),
 // outputs, groups of the gate).
 struct NormOuts {
   float* out[5];
 };
-__global__ __launch_bounds__(256) void k_norm_params(const float* __restrict__ part, const float* __restrict__ gpart,
-                                                     int wgs, int groups, int split, int W, NormOuts O) {
-  __shared__ float buf[16][17];
+__global__ __launch_bounds__(1024) void k_norm_params(const float* __restrict__ part, const float* __restrict__ gpart,
+                                                      int wgs, int split, int W, NormOuts O) {
+  __shared__ float buf[64][17];
   const int which = blockIdx.y;
   float* out = O.out[which];
   if (!out || (which != 4 && blockIdx.z > 0)) return;
@@ -435,14 +512,16 @@ __global__ __launch_bounds__(256) void k_norm_params(const float* __restrict__ p
   const int count = which == 4 ? split : wgs;
   const int cl = threadIdx.x & 15, s = threadIdx.x >> 4, col = blockIdx.x * 16 + cl;
   float v = 0.f;
-  if (col < W)
-    for (int p = s; p < count; p += 16) v += src[p * stride + col];
+  if (col < W) {
+#pragma unroll 8
+    for (int p = s; p < count; p += 64) v += src[p * stride + col];
+  }
   buf[s][cl] = v;
   __syncthreads();
   if (s == 0 && col < W) {
     float t = 0.f;
 #pragma unroll
-    for (int k = 0; k < 16; ++k) t += buf[k][cl];
+    for (int k = 0; k < 64; ++k) t += buf[k][cl];
     out[(which == 4 ? (int64_t)blockIdx.z * W : 0) + col] = t;
   }
 }
@@ -453,20 +532,22 @@ int threads_per_row(int W) {
   return t;
 }
 
-// The gradient's grouping of rows into workgroups.  One workgroup's sums cost
-// a pass over its rows' registers at the end, so there are only as many as
-// fill the compute units twice; a gate per batch keeps a workgroup inside one
-// batch, or gives it several whole ones where batches are many.
-constexpr int kNormWgs = 512;
+// The gradient's grouping of rows into workgroups: as many as are resident at
+// once (the registers hold two waves per SIMD), since each writes a row of
+// parameter sums (D = 4096: 102 us with 256 workgroups of 512 threads, 112 with
+// 512; D = 1024: 81 us with 512 of 256, 109 with 256).  A gate per batch keeps a
+// workgroup inside one batch, or gives it several whole ones where batches are
+// many.
+int norm_wgs(int tpr) { return tpr > 256 ? 256 : 512; }
 NormParts parts_of(const NormDims& d) {
   NormParts p{};
   p.groups = d.gate_batches > 1 ? d.gate_batches : 1;
   p.group_rows = d.gate_batches > 1 ? d.n : (int64_t)d.B * d.n;
   const int tpr = threads_per_row(d.W), teams = wg_threads(tpr) / tpr;
   const int64_t most = (p.group_rows + teams - 1) / teams;
-  int64_t split = kNormWgs / p.groups;
+  int64_t split = norm_wgs(tpr) / p.groups;
   p.split = (int)(split < 1 ? 1 : (split > most ? most : split));
-  p.each = p.split > 1 ? 1 : (p.groups + kNormWgs - 1) / kNormWgs;
+  p.each = p.split > 1 ? 1 : (p.groups + norm_wgs(tpr) - 1) / norm_wgs(tpr);
   return p;
 }
 int wgs_of(const NormParts& p) { return p.split > 1 ? p.groups * p.split : (p.groups + p.each - 1) / p.each; }
@@ -535,9 +616,16 @@ hipError_t launch_norm_grad(const NormDims& d, const NormTensors& t, const void*
   {
     TimedLaunch tl("norm_grad", st);
 #define GA_CALL(DT, TPR, VEC)                                                                                     \
-  hipLaunchKernelGGL((k_norm_grad<DT, TPR, VEC>), dim3((unsigned)wgs), dim3(wg_threads(TPR)), 0, st,               \
-                     args_of<DT>(d, t), (const typename DT::T*)dY, (const typename DT::T*)dH, (typename DT::T*)dX, \
-                     (typename DT::T*)dF, p)
+  do {                                                                                                             \
+    if (out[1] || out[3])                                                                                          \
+      hipLaunchKernelGGL((k_norm_grad<DT, TPR, VEC, true>), dim3((unsigned)wgs), dim3(wg_threads(TPR)), 0, st,      \
+                         args_of<DT>(d, t), (const typename DT::T*)dY, (const typename DT::T*)dH,                  \
+                         (typename DT::T*)dX, (typename DT::T*)dF, p);                                             \
+    else                                                                                                           \
+      hipLaunchKernelGGL((k_norm_grad<DT, TPR, VEC, false>), dim3((unsigned)wgs), dim3(wg_threads(TPR)), 0, st,     \
+                         args_of<DT>(d, t), (const typename DT::T*)dY, (const typename DT::T*)dH,                  \
+                         (typename DT::T*)dX, (typename DT::T*)dF, p);                                             \
+  } while (0)
     GA_NORM_ALL(GA_CALL)
 #undef GA_CALL
   }
@@ -545,8 +633,8 @@ hipError_t launch_norm_grad(const NormDims& d, const NormTensors& t, const void*
   if (params || gate) {
     TimedLaunch tl("norm_params", st);
     NormOuts o{{out[0], out[1], out[2], out[3], gate ? out[4] : nullptr}};
-    hipLaunchKernelGGL(k_norm_params, dim3((unsigned)((d.W + 15) / 16), 5, gate ? (unsigned)p.groups : 1u), dim3(256),
-                       0, st, p.part, p.gpart, wgs, p.groups, p.split, d.W, o);
+    hipLaunchKernelGGL(k_norm_params, dim3((unsigned)((d.W + 15) / 16), 5, gate ? (unsigned)p.groups : 1u), dim3(1024),
+                       0, st, p.part, p.gpart, wgs, p.split, d.W, o);
   }
   return hipGetLastError();
 }

@@ -26,22 +26,23 @@ namespace {
 constexpr int kTok = 64;  // tokens per workgroup: four threads each, eight pairs a thread
 
 template <class DT>
-struct Half8 {
-  float v[8];
+struct Half8 {  // eight values as stored
+  static constexpr int kWords = DT::kBits == 16 ? 1 : 2;
+  u32x4 w[kWords];
   __device__ __forceinline__ void load(const typename DT::T* p) {
-    if constexpr (DT::kBits == 16) {
-      const u32x4 w = *(const u32x4*)p;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        v[2 * e] = bf16_to_f32(w[e] & 0xffffu);
-        v[2 * e + 1] = bf16_to_f32(w[e] >> 16);
-      }
-    } else {
-      const float4 a = *(const float4*)p, b = *(const float4*)(p + 4);
-      v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+    for (int i = 0; i < kWords; ++i) w[i] = ((const u32x4*)p)[i];
+  }
+  __device__ __forceinline__ void get(float (&v)[8]) const {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      if constexpr (DT::kBits == 16)
+        v[e] = __uint_as_float(e & 1 ? w[0][e / 2] & 0xffff0000u : w[0][e / 2] << 16);
+      else
+        v[e] = __uint_as_float(w[e / 4][e % 4]);
     }
   }
-  __device__ __forceinline__ void store(typename DT::T* p) const {
+  static __device__ __forceinline__ void store(typename DT::T* p, const float (&v)[8]) {
     if constexpr (DT::kBits == 16) {
       u32x4 w;
 #pragma unroll
@@ -74,25 +75,40 @@ __global__ __launch_bounds__(256) void k_rotary(const typename DT::T* Q, const t
     sincospif(2.0f * f, &si[e], &co[e]);
   }
   const int lo = INTERLEAVED ? 16 * s : 8 * s, hi = INTERLEAVED ? 16 * s + 8 : 32 + 8 * s;
+  // a head's row is requested before the last one's turn is written
+  auto row = [&](int h, bool& q) __attribute__((always_inline)) {
+    q = h < H;
+    return ((q ? b * H + h : b * Hk + (h - H)) * n + t) * 64;
+  };
+  Half8<DT> nu, nw;
+  auto request = [&](int h) __attribute__((always_inline)) {
+    if (h >= H + Hk) return;
+    bool q;
+    const int64_t at = row(h, q);
+    const typename DT::T* src = (q ? Q : K) + at;
+    nu.load(src + lo);
+    nw.load(src + hi);
+  };
+  request(blockIdx.y);
   for (int h = blockIdx.y; h < H + Hk; h += gridDim.y) {
-    const bool q = h < H;
-    const int64_t row = ((q ? b * H + h : b * Hk + (h - H)) * n + t) * 64;
-    const typename DT::T* src = (q ? Q : K) + row;
-    typename DT::T* dst = (q ? Qo : Ko) + row;
-    Half8<DT> u, w;
-    u.load(src + lo);
-    w.load(src + hi);
+    float u[8], w[8];
+    nu.get(u);
+    nw.get(w);
+    request(h + gridDim.y);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       // interleaved: pair e is (2e, 2e + 1) of the sixteen values u, w; halves: (u[e], w[e])
-      float& x = INTERLEAVED ? (e < 4 ? u.v[2 * e] : w.v[2 * e - 8]) : u.v[e];
-      float& y = INTERLEAVED ? (e < 4 ? u.v[2 * e + 1] : w.v[2 * e - 7]) : w.v[e];
+      float& x = INTERLEAVED ? (e < 4 ? u[2 * e] : w[2 * e - 8]) : u[e];
+      float& y = INTERLEAVED ? (e < 4 ? u[2 * e + 1] : w[2 * e - 7]) : w[e];
       const float a = x, c = y;
       x = a * co[e] - c * si[e];
       y = c * co[e] + a * si[e];
     }
-    u.store(dst + lo);
-    w.store(dst + hi);
+    bool q;
+    const int64_t at = row(h, q);
+    typename DT::T* dst = (q ? Qo : Ko) + at;
+    Half8<DT>::store(dst + lo, u);
+    Half8<DT>::store(dst + hi, w);
   }
 }
 
