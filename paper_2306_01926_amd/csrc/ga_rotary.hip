@@ -23,92 +23,103 @@ namespace {
 
 #include "ga_device.h"
 
-constexpr int kTok = 64;  // tokens per workgroup: four threads each, eight pairs a thread
+// A thread takes 16 bytes of a row, so that a wave's loads are whole rows
+// (107 us at B H = 128, n = 8000 against 110 with two loads of half rows).
+// Interleaved, its values are pairs; in the halves' layout they are one side of
+// as many pairs, whose other side the mirrored thread of the row holds: thread s
+// of T has values kPer s of the first half, thread T - 1 - s those of the second.
+template <class DT, bool INTERLEAVED>
+struct Tile {
+  static constexpr int kPer = 128 / DT::kBits;  // values in 16 bytes
+  static constexpr int kPairs = INTERLEAVED ? kPer / 2 : kPer;
+  static constexpr int kThreads = 64 / kPer;      // threads per token: 8 (bf16) or 16
+  static constexpr int kTokens = 256 / kThreads;  // tokens per workgroup
+  u32x4 w;
 
-template <class DT>
-struct Half8 {  // eight values as stored
-  static constexpr int kWords = DT::kBits == 16 ? 1 : 2;
-  u32x4 w[kWords];
-  __device__ __forceinline__ void load(const typename DT::T* p) {
-#pragma unroll
-    for (int i = 0; i < kWords; ++i) w[i] = ((const u32x4*)p)[i];
+  static __device__ __forceinline__ bool second(int s) { return !INTERLEAVED && s >= kThreads / 2; }
+  static __device__ __forceinline__ int pair0(int s) { return kPairs * (second(s) ? kThreads - 1 - s : s); }
+  static __device__ __forceinline__ int offset(int s) {
+    return INTERLEAVED ? kPer * s : pair0(s) + (second(s) ? 32 : 0);
   }
-  __device__ __forceinline__ void get(float (&v)[8]) const {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      if constexpr (DT::kBits == 16)
-        v[e] = __uint_as_float(e & 1 ? w[0][e / 2] & 0xffff0000u : w[0][e / 2] << 16);
-      else
-        v[e] = __uint_as_float(w[e / 4][e % 4]);
-    }
+  __device__ __forceinline__ void load(const typename DT::T* p) { w = *(const u32x4*)p; }
+  static __device__ __forceinline__ float value(const u32x4& w, int e) {
+    if constexpr (DT::kBits == 16)
+      return __uint_as_float(e & 1 ? w[e / 2] & 0xffff0000u : w[e / 2] << 16);
+    else
+      return __uint_as_float(w[e]);
   }
-  static __device__ __forceinline__ void store(typename DT::T* p, const float (&v)[8]) {
-    if constexpr (DT::kBits == 16) {
-      u32x4 w;
+  // halves: si is negated in the first half's threads
+  __device__ __forceinline__ void turn(const float (&co)[kPairs], const float (&si)[kPairs], typename DT::T* p) const {
+    float v[kPer];
+    if constexpr (INTERLEAVED) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) w[e] = pack_bf16x2(v[2 * e], v[2 * e + 1]);
-      *(u32x4*)p = w;
+      for (int m = 0; m < kPairs; ++m) {
+        const float a = value(w, 2 * m), c = value(w, 2 * m + 1);
+        v[2 * m] = a * co[m] - c * si[m];
+        v[2 * m + 1] = c * co[m] + a * si[m];
+      }
     } else {
-      *(float4*)p = make_float4(v[0], v[1], v[2], v[3]);
-      *(float4*)(p + 4) = make_float4(v[4], v[5], v[6], v[7]);
+      u32x4 o;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] = (uint32_t)dpp<kThreads == 8 ? kHalfMirror : kMirror>((int)w[e]);
+#pragma unroll
+      for (int m = 0; m < kPairs; ++m) v[m] = value(w, m) * co[m] + value(o, m) * si[m];
     }
+    u32x4 o;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if constexpr (DT::kBits == 16)
+        o[e] = pack_bf16x2(v[2 * e], v[2 * e + 1]);
+      else
+        o[e] = __float_as_uint(v[e]);
+    }
+    *(u32x4*)p = o;
   }
 };
 
-// grid (ceil(n / 64), head shares, B).  Workgroup y takes heads y, y + gridDim.y, ...
+// grid (ceil(n / kTokens), head shares, B).  Workgroup y takes heads y, y + gridDim.y, ...
 // of the H query heads followed by the Hk key heads.
 template <class DT, bool INTERLEAVED>
 __global__ __launch_bounds__(256) void k_rotary(const typename DT::T* Q, const typename DT::T* K, const void* pos,
                                                 RotaryPlan P, int H, int Hk, int n, typename DT::T* Qo,
                                                 typename DT::T* Ko) {
-  const int t = blockIdx.x * kTok + (threadIdx.x >> 2), s = threadIdx.x & 3;
+  using R = Tile<DT, INTERLEAVED>;
+  const int t = blockIdx.x * R::kTokens + threadIdx.x / R::kThreads, s = threadIdx.x % R::kThreads;
   if (t >= n) return;
   const int64_t b = blockIdx.z, pb = P.pos_batches > 1 ? b : 0;
-  float co[8], si[8];
+  // a head's row is requested two heads before its turn is written, the first
+  // ones before the angles are formed
+  auto row = [&](int h) __attribute__((always_inline)) {
+    return ((h < H ? b * H + h : b * Hk + (h - H)) * n + t) * 64 + R::offset(s);
+  };
+  const int step = gridDim.y, heads = H + Hk;
+  R x[2];
+  auto request = [&](int h, R& to) __attribute__((always_inline)) {
+    if (h < heads) to.load((h < H ? Q : K) + row(h));
+  };
+  request(blockIdx.y, x[0]);
+  request(blockIdx.y + step, x[1]);
+  float co[R::kPairs], si[R::kPairs];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const int i = 8 * s + e;
+  for (int e = 0; e < R::kPairs; ++e) {
+    const int i = R::pair0(s) + e;
     const int64_t at = ((int64_t)P.axis[i] * P.pos_batches + pb) * n + t;
     const double x = P.pos_float ? (double)((const float*)pos)[at] : (double)((const int32_t*)pos)[at];
     const double turns = x * P.turns[i];
     const float f = (float)(turns - rint(turns));  // [-1/2, 1/2]
-    sincospif(2.0f * f, &si[e], &co[e]);
+    si[e] = __builtin_amdgcn_sinf(f);  // of f turns; off by at most 2^-23 there (measured over 2^22 values)
+    co[e] = __builtin_amdgcn_cosf(f);
+    if (!INTERLEAVED && !R::second(s)) si[e] = -si[e];
   }
-  const int lo = INTERLEAVED ? 16 * s : 8 * s, hi = INTERLEAVED ? 16 * s + 8 : 32 + 8 * s;
-  // a head's row is requested before the last one's turn is written
-  auto row = [&](int h, bool& q) __attribute__((always_inline)) {
-    q = h < H;
-    return ((q ? b * H + h : b * Hk + (h - H)) * n + t) * 64;
-  };
-  Half8<DT> nu, nw;
-  auto request = [&](int h) __attribute__((always_inline)) {
-    if (h >= H + Hk) return;
-    bool q;
-    const int64_t at = row(h, q);
-    const typename DT::T* src = (q ? Q : K) + at;
-    nu.load(src + lo);
-    nw.load(src + hi);
-  };
-  request(blockIdx.y);
-  for (int h = blockIdx.y; h < H + Hk; h += gridDim.y) {
-    float u[8], w[8];
-    nu.get(u);
-    nw.get(w);
-    request(h + gridDim.y);
+  for (int h = blockIdx.y; h < heads; h += 2 * step) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      // interleaved: pair e is (2e, 2e + 1) of the sixteen values u, w; halves: (u[e], w[e])
-      float& x = INTERLEAVED ? (e < 4 ? u[2 * e] : w[2 * e - 8]) : u[e];
-      float& y = INTERLEAVED ? (e < 4 ? u[2 * e + 1] : w[2 * e - 7]) : w[e];
-      const float a = x, c = y;
-      x = a * co[e] - c * si[e];
-      y = c * co[e] + a * si[e];
+    for (int u = 0; u < 2; ++u) {
+      const int g = h + u * step;
+      if (g >= heads) break;
+      const R now = x[u];
+      request(g + 2 * step, x[u]);
+      now.turn(co, si, (g < H ? Qo : Ko) + row(g));
     }
-    bool q;
-    const int64_t at = row(h, q);
-    typename DT::T* dst = (q ? Qo : Ko) + at;
-    Half8<DT>::store(dst + lo, u);
-    Half8<DT>::store(dst + hi, w);
   }
 }
 
@@ -116,12 +127,14 @@ __global__ __launch_bounds__(256) void k_rotary(const typename DT::T* Q, const t
 
 hipError_t launch_rotary(int dtype, int B, int H, int Hk, int n, const void* Q, const void* K, const void* pos,
                          const RotaryPlan& plan, bool interleaved, void* Qo, void* Ko, hipStream_t st) {
-  const unsigned tiles = (unsigned)((n + kTok - 1) / kTok);
+  const int tokens = dtype == 1 ? (interleaved ? Tile<BF16, true>::kTokens : Tile<BF16, false>::kTokens)
+                                : (interleaved ? Tile<F32, true>::kTokens : Tile<F32, false>::kTokens);
+  const unsigned tiles = (unsigned)((n + tokens - 1) / tokens);
   const int heads = H + Hk;
   // the sines are formed once per workgroup, so a workgroup takes every head of
   // its tokens unless that leaves compute units idle
   const int64_t wgs = (int64_t)tiles * B;
-  int64_t shares = (2048 + wgs - 1) / wgs;
+  int64_t shares = (1024 + wgs - 1) / wgs;
   if (shares > heads) shares = heads;
   const dim3 grid(tiles, (unsigned)shares, (unsigned)B);
   TimedLaunch tl("rotary", st);

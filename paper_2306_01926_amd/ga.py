@@ -8,6 +8,7 @@ CPU fallback: if the library is missing the call raises.
 from __future__ import annotations
 
 import ctypes
+import functools
 import math
 import os
 
@@ -423,39 +424,55 @@ def backward(Q: torch.Tensor, dO: torch.Tensor, belong: torch.Tensor, centroid: 
 def _launch(dev, call, *args) -> None:
     """One entry point on the current stream of `dev`, with that device current."""
     if dev.index is None or dev.index == torch.cuda.current_device():
-        _check(call(*args, _stream(dev)))
-        return
-    with torch.cuda.device(dev):
-        _check(call(*args, _stream(dev)))
+        rc = call(*args, _stream_handle(dev))
+    else:
+        with torch.cuda.device(dev):
+            rc = call(*args, _stream_handle(dev))
+    if rc:
+        _check(rc)
+
+
+def _at(t, name: str, dev, dtype, shape):
+    """Address of a tensor that _expect accepts (which says what is wrong with another one).  The smallest calls are
+    bound by the host: each check is made once, in one expression."""
+    if not (isinstance(t, torch.Tensor) and t.dtype is dtype and t.device == dev and t.shape == shape
+            and t.is_contiguous()):
+        _expect(t, name, dev, dtype, shape)
+    return t.data_ptr()
+
+
+def _maybe(t, name: str, dev, dtype, shape):
+    """_at, or NULL for None."""
+    return None if t is None else _at(t, name, dev, dtype, shape)
 
 
 def _scratch(nbytes: int, dev, ws):
-    """(pointer, bytes) of a workspace: the caller's, or one of this call's own (so that captured graphs and
-    streams never share one).  The tensor is returned too, to live until the launch is enqueued."""
+    """(tensor, address, bytes) of a workspace: the caller's, or one of this call's own (so that captured graphs and
+    streams never share one).  The tensor is to live until the launch is enqueued."""
     if ws is None:
         if nbytes == 0:
             return None, None, 0
         ws = torch.empty(nbytes, dtype=torch.uint8, device=dev)
     else:
         _expect(ws, "ws", dev, torch.uint8)
-    return ws, _p(ws), ws.numel()
+    return ws, ws.data_ptr(), ws.numel()
 
 
-def _linear_args(Q, K, V, log_decay, lengths, state):
-    """Checks shared by the linear attention's calls; (shape, Hk, device, state shape)."""
+@functools.lru_cache(maxsize=1024)
+def _linear_shape(B: int, H: int, Hk: int, n: int, d: int, dtype):
+    """(shape, forward workspace, backward workspace) of a call (the sizes depend on nothing else)."""
+    s = Shape(B, H, n, d, {torch.bfloat16: GA_BF16, torch.float32: GA_F32}[dtype])
+    return s, int(lib().ga_linear_workspace_bytes(s, Hk)), int(lib().ga_linear_backward_workspace_bytes(s, Hk))
+
+
+def _heads(Q, K, name: str):
+    """(B, H, Hk, n, d, device, dtype) of queries [B,H,n,d] and keys [B,Hk,n,d]."""
     dev = _qkv_like(Q, "Q")
-    s = shape_of(Q)
-    _expect(Q, "Q", dev, Q.dtype)
     if not isinstance(K, torch.Tensor) or K.dim() != 4:
-        raise ValueError("K must be a [B, Hk, n, d] tensor")
+        raise ValueError(f"{name} must be a [B, Hk, n, d] tensor")
+    _dtype_code(Q)
     B, H, n, d = Q.shape
-    Hk = K.shape[1]
-    _expect(K, "K", dev, Q.dtype, (B, Hk, n, d))
-    _expect(V, "V", dev, Q.dtype, (B, Hk, n, d))
-    _expect(log_decay, "log_decay", dev, torch.float32, (H,))
-    _expect(lengths, "lengths", dev, torch.int32, (B,), optional=True)
-    _expect(state, "state", dev, torch.float32, (B, H, d, d), optional=True)
-    return s, Hk, dev, (B, H, d, d)
+    return B, H, K.shape[1], n, d, dev, Q.dtype
 
 
 def linear_workspace_bytes(shape: Shape, Hk: int) -> int:
@@ -469,16 +486,19 @@ def linear_attend(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, log_decay: 
     """Causal linear attention with a decay per head: O [B,H,n,64], or (O, state [B,H,64,64] fp32) if return_state.
     K, V [B,Hk,n,64]; log_decay [H] fp32; lengths [B] int32; state: the state before the first token (out_state may
     be that tensor itself)."""
-    s, Hk, dev, states = _linear_args(Q, K, V, log_decay, lengths, state)
-    _expect(out, "out", dev, Q.dtype, Q.shape, optional=True)
-    _expect(out_state, "out_state", dev, torch.float32, states, optional=True)
-    scale = 1.0 / math.sqrt(Q.shape[3]) if scale is None else float(scale)
+    B, H, Hk, n, d, dev, dt = _heads(Q, K, "K")
+    q, kv, states = (B, H, n, d), (B, Hk, n, d), (B, H, d, d)
+    pointers = (_at(Q, "Q", dev, dt, q), _at(K, "K", dev, dt, kv), _at(V, "V", dev, dt, kv),
+                _at(log_decay, "log_decay", dev, torch.float32, (H,)),
+                _maybe(lengths, "lengths", dev, torch.int32, (B,)),
+                _maybe(state, "state", dev, torch.float32, states))
     O = torch.empty_like(Q) if out is None else out
     if return_state and out_state is None:
         out_state = torch.empty(states, dtype=torch.float32, device=dev)
-    ws, wp, nb = _scratch(lib().ga_linear_workspace_bytes(s, Hk), dev, ws)
-    _launch(dev, lib().ga_linear_attend, s, Hk, _p(Q), _p(K), _p(V), _p(log_decay), _p(lengths), _p(state), scale,
-            _p(O), _p(out_state), wp, nb)
+    s, nbytes, _ = _linear_shape(B, H, Hk, n, d, dt)
+    ws, wp, nb = _scratch(nbytes, dev, ws)
+    _launch(dev, lib().ga_linear_attend, s, Hk, *pointers, 1.0 / math.sqrt(d) if scale is None else float(scale),
+            _at(O, "out", dev, dt, q), _maybe(out_state, "out_state", dev, torch.float32, states), wp, nb)
     return (O, out_state) if return_state else O
 
 
@@ -492,15 +512,19 @@ def linear_backward(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, dO: torch
                     return_dstate: bool = False, ws=None):
     """Gradient of linear_attend: (dQ, dK, dV), and the initial state's gradient if return_dstate.  dstate: the
     gradient that reaches the final state."""
-    s, Hk, dev, states = _linear_args(Q, K, V, log_decay, lengths, state)
-    _expect(dO, "dO", dev, Q.dtype, Q.shape)
-    _expect(dstate, "dstate", dev, torch.float32, states, optional=True)
-    scale = 1.0 / math.sqrt(Q.shape[3]) if scale is None else float(scale)
+    B, H, Hk, n, d, dev, dt = _heads(Q, K, "K")
+    q, kv, states = (B, H, n, d), (B, Hk, n, d), (B, H, d, d)
+    pointers = (_at(Q, "Q", dev, dt, q), _at(K, "K", dev, dt, kv), _at(V, "V", dev, dt, kv), _at(dO, "dO", dev, dt, q),
+                _at(log_decay, "log_decay", dev, torch.float32, (H,)),
+                _maybe(lengths, "lengths", dev, torch.int32, (B,)),
+                _maybe(state, "state", dev, torch.float32, states),
+                _maybe(dstate, "dstate", dev, torch.float32, states))
     dQ, dK, dV = torch.empty_like(Q), torch.empty_like(K), torch.empty_like(V)
     out = torch.empty(states, dtype=torch.float32, device=dev) if return_dstate else None
-    ws, wp, nb = _scratch(lib().ga_linear_backward_workspace_bytes(s, Hk), dev, ws)
-    _launch(dev, lib().ga_linear_backward, s, Hk, _p(Q), _p(K), _p(V), _p(dO), _p(log_decay), _p(lengths), _p(state),
-            _p(dstate), scale, _p(dQ), _p(dK), _p(dV), _p(out), wp, nb)
+    s, _, nbytes = _linear_shape(B, H, Hk, n, d, dt)
+    ws, wp, nb = _scratch(nbytes, dev, ws)
+    _launch(dev, lib().ga_linear_backward, s, Hk, *pointers, 1.0 / math.sqrt(d) if scale is None else float(scale),
+            dQ.data_ptr(), dK.data_ptr(), dV.data_ptr(), None if out is None else out.data_ptr(), wp, nb)
     return (dQ, dK, dV, out) if return_dstate else (dQ, dK, dV)
 
 
@@ -509,21 +533,28 @@ def linear_step(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, log_decay: to
                 out_state: torch.Tensor | None = None):
     """One token per sequence (Q [B,H,1,64]) on kept states [states,H,64,64] fp32, updated in place unless out_state
     is given: (O, the updated states).  slots [B] int32: the state of each batch row (outside the states: padding)."""
-    s, Hk, dev, _ = _linear_args(Q, K, V, log_decay, slots, None)
+    B, H, Hk, n, d, dev, dt = _heads(Q, K, "K")
     if not isinstance(state, torch.Tensor) or state.dim() != 4:
         raise ValueError("state must be a [states, H, 64, 64] tensor")
-    _expect(state, "state", dev, torch.float32, (state.shape[0], Q.shape[1], Q.shape[3], Q.shape[3]))
-    _expect(out_state, "out_state", dev, torch.float32, state.shape, optional=True)
-    _expect(out, "out", dev, Q.dtype, Q.shape, optional=True)
-    scale = 1.0 / math.sqrt(Q.shape[3]) if scale is None else float(scale)
+    many = state.shape[0]
+    q, kv, states = (B, H, n, d), (B, Hk, n, d), (many, H, d, d)
     O = torch.empty_like(Q) if out is None else out
-    out_state = state if out_state is None else out_state
-    _launch(dev, lib().ga_linear_step, s, Hk, _p(Q), _p(K), _p(V), _p(log_decay), _p(slots), state.shape[0],
-            _p(state), scale, _p(O), _p(out_state))
+    if out_state is None:
+        out_state = state
+    _launch(dev, lib().ga_linear_step, _linear_shape(B, H, Hk, n, d, dt)[0], Hk, _at(Q, "Q", dev, dt, q),
+            _at(K, "K", dev, dt, kv), _at(V, "V", dev, dt, kv), _at(log_decay, "log_decay", dev, torch.float32, (H,)),
+            _maybe(slots, "slots", dev, torch.int32, (B,)), many, _at(state, "state", dev, torch.float32, states),
+            1.0 / math.sqrt(d) if scale is None else float(scale), _at(O, "out", dev, dt, q),
+            _at(out_state, "out_state", dev, torch.float32, states))
     return O, out_state
 
 
 ROTARY_INTERLEAVED, ROTARY_SHARED, ROTARY_INVERSE, ROTARY_FLOAT_POS = 1, 2, 4, 8
+
+
+@functools.lru_cache(maxsize=64)
+def _pairs(pairs: tuple):
+    return (ctypes.c_int32 * max(1, len(pairs)))(*pairs)
 
 
 def rotary(Q: torch.Tensor, K: torch.Tensor | None, pos: torch.Tensor, pairs, base: float = 10000.0,
@@ -532,30 +563,21 @@ def rotary(Q: torch.Tensor, K: torch.Tensor | None, pos: torch.Tensor, pairs, ba
     pos [axes, B or 1, n] int32 or fp32; pairs: the feature pairs of each axis; shared: one ladder of frequencies over
     all pairs instead of one per axis; inverse: the opposite turn, which is the gradient.  out: (Q', K') to write,
     which may be Q and K themselves."""
-    dev = _qkv_like(Q, "Q")
-    s = shape_of(Q)
-    B, H, n, d = Q.shape
+    B, H, Hk, n, d, dev, dt = _heads(Q, Q if K is None else K, "K")
     pairs = tuple(int(p) for p in pairs)
-    _expect(Q, "Q", dev, Q.dtype)
-    Hk = H
-    if K is not None:
-        if not isinstance(K, torch.Tensor) or K.dim() != 4:
-            raise ValueError("K must be a [B, Hk, n, d] tensor")
-        Hk = K.shape[1]
-        _expect(K, "K", dev, Q.dtype, (B, Hk, n, d))
     if not isinstance(pos, torch.Tensor) or pos.dim() != 3 or pos.shape[1] not in (1, B):
         raise ValueError(f"pos must be an [axes, 1 or {B}, n] tensor")
-    if pos.dtype not in (torch.int32, torch.float32):
+    floats = pos.dtype is torch.float32
+    if not floats and pos.dtype is not torch.int32:
         raise ValueError(f"pos has dtype {pos.dtype}, expected int32 or float32")
-    _expect(pos, "pos", dev, pos.dtype, (len(pairs), pos.shape[1], n))
+    q, k, many = (B, H, n, d), (B, Hk, n, d), pos.shape[1]
     Qo, Ko = (torch.empty_like(Q), None if K is None else torch.empty_like(K)) if out is None else out
-    _expect(Qo, "out[0]", dev, Q.dtype, Q.shape)
-    if K is not None:
-        _expect(Ko, "out[1]", dev, Q.dtype, K.shape)
     flags = (ROTARY_INTERLEAVED * bool(interleaved) + ROTARY_SHARED * bool(shared) + ROTARY_INVERSE * bool(inverse)
-             + ROTARY_FLOAT_POS * (pos.dtype == torch.float32))
-    _launch(dev, lib().ga_rotary, s, Hk, _p(Q), _p(K), _p(pos), pos.shape[1], len(pairs),
-            (ctypes.c_int32 * len(pairs))(*pairs), float(base), flags, _p(Qo), _p(Ko))
+             + ROTARY_FLOAT_POS * floats)
+    _launch(dev, lib().ga_rotary, _linear_shape(B, H, Hk, n, d, dt)[0], Hk, _at(Q, "Q", dev, dt, q),
+            None if K is None else _at(K, "K", dev, dt, k), _at(pos, "pos", dev, pos.dtype, (len(pairs), many, n)),
+            many, len(pairs), _pairs(pairs), float(base), flags, _at(Qo, "out[0]", dev, dt, q),
+            None if K is None else _at(Ko, "out[1]", dev, dt, k))
     return Qo if K is None else (Qo, Ko)
 
 
@@ -563,27 +585,24 @@ NORMS = {"rms": 0, "layer": 1}
 
 
 def _norm_args(X, F, norm, eps, post_weight, post_bias, gate, pre_weight, pre_bias, residual_scale, branch_scale):
-    """Checks shared by the norm's calls; (ga_norm_t, device, the tensors' pointers)."""
+    """Checks shared by the norm's calls; (ga_norm_t, device, dtype, the tensors' addresses)."""
     if not isinstance(X, torch.Tensor) or X.dim() != 3:
         raise ValueError("X must be a [B, n, D] tensor")
     if norm not in NORMS:
         raise ValueError(f"norm must be one of {sorted(NORMS)} (got {norm!r})")
-    dev = _device_of(X)
+    dev, dt, code = _device_of(X), X.dtype, _dtype_code(X)
     B, n, D = X.shape
-    code = _dtype_code(X)
-    _expect(X, "X", dev, X.dtype)
-    _expect(F, "F", dev, X.dtype, X.shape, optional=True)
-    for t, name in ((post_weight, "post_weight"), (post_bias, "post_bias"), (pre_weight, "pre_weight"),
-                    (pre_bias, "pre_bias")):
-        _expect(t, name, dev, X.dtype, (D,), optional=True)
-    batches = 0
+    batches, g = 0, None
     if gate is not None:
         if not isinstance(gate, torch.Tensor) or gate.dim() not in (1, 2):
             raise ValueError("gate must be a [D] or [B, D] tensor")
         batches = 1 if gate.dim() == 1 else B
-        _expect(gate, "gate", dev, X.dtype, (D,) if gate.dim() == 1 else (B, D))
+        g = _at(gate, "gate", dev, dt, (D,) if gate.dim() == 1 else (B, D))
     s = Norm(B, n, D, code, NORMS[norm], batches, eps, residual_scale, branch_scale)
-    return s, dev, [_p(t) for t in (X, F, post_weight, post_bias, gate, pre_weight, pre_bias)]
+    w = (D,)
+    return s, dev, dt, (_at(X, "X", dev, dt, (B, n, D)), _maybe(F, "F", dev, dt, (B, n, D)),
+                        _maybe(post_weight, "post_weight", dev, dt, w), _maybe(post_bias, "post_bias", dev, dt, w), g,
+                        _maybe(pre_weight, "pre_weight", dev, dt, w), _maybe(pre_bias, "pre_bias", dev, dt, w))
 
 
 def norm_residual(X: torch.Tensor, F: torch.Tensor | None = None, norm: str = "rms", eps: float = 1e-6,
@@ -592,11 +611,12 @@ def norm_residual(X: torch.Tensor, F: torch.Tensor | None = None, norm: str = "r
     """Y = residual_scale X + branch_scale gate * post_norm(F) and, with pre_weight, H = pre_norm(Y): returns Y,
     (Y, H), or H alone without return_sum.  X, F [B,n,D]; weights and biases [D]; gate [D] or [B,D]; norm "rms" or
     "layer"; no post_weight: F itself; no F: the residual stream alone."""
-    s, dev, tensors = _norm_args(X, F, norm, eps, post_weight, post_bias, gate, pre_weight, pre_bias, residual_scale,
-                                 branch_scale)
+    s, dev, _, tensors = _norm_args(X, F, norm, eps, post_weight, post_bias, gate, pre_weight, pre_bias,
+                                    residual_scale, branch_scale)
     Y = torch.empty_like(X) if return_sum else None
     H = torch.empty_like(X) if pre_weight is not None else None
-    _launch(dev, lib().ga_norm_residual, s, *tensors, _p(Y), _p(H))
+    _launch(dev, lib().ga_norm_residual, s, *tensors, None if Y is None else Y.data_ptr(),
+            None if H is None else H.data_ptr())
     return H if Y is None else Y if H is None else (Y, H)
 
 
@@ -610,10 +630,9 @@ def norm_residual_backward(X: torch.Tensor, F: torch.Tensor | None, dY: torch.Te
                            branch_scale: float = 1.0, ws=None) -> dict:
     """Gradient of norm_residual from those of Y and H (each may be None): a dict of dX, dF (X's dtype) and, for what
     the call has, dpost_w, dpost_b, dgate, dpre_w, dpre_b (fp32 sums over the tokens)."""
-    s, dev, tensors = _norm_args(X, F, norm, eps, post_weight, post_bias, gate, pre_weight, pre_bias, residual_scale,
-                                 branch_scale)
-    _expect(dY, "dY", dev, X.dtype, X.shape, optional=True)
-    _expect(dH, "dH", dev, X.dtype, X.shape, optional=True)
+    s, dev, dt, tensors = _norm_args(X, F, norm, eps, post_weight, post_bias, gate, pre_weight, pre_bias,
+                                     residual_scale, branch_scale)
+    dYp, dHp = (_maybe(t, name, dev, dt, X.shape) for t, name in ((dY, "dY"), (dH, "dH")))
     B, _, D = X.shape
     empty = torch.empty if B else torch.zeros  # no tokens: nothing is enqueued, every sum is zero
 
@@ -625,7 +644,8 @@ def norm_residual_backward(X: torch.Tensor, F: torch.Tensor | None, dY: torch.Te
                dgate=None if gate is None else sums(True, *gate.shape),
                dpre_w=sums(dH is not None, D), dpre_b=sums(dH is not None and pre_bias is not None, D))
     ws, wp, nb = _scratch(lib().ga_norm_backward_workspace_bytes(s), dev, ws)
-    _launch(dev, lib().ga_norm_residual_backward, s, *tensors, _p(dY), _p(dH), *(_p(t) for t in got.values()), wp, nb)
+    _launch(dev, lib().ga_norm_residual_backward, s, *tensors, dYp, dHp,
+            *(None if t is None else t.data_ptr() for t in got.values()), wp, nb)
     return {k: t for k, t in got.items() if t is not None}
 
 
