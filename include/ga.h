@@ -279,7 +279,9 @@ int ga_backward(ga_shape_t s, const void *Q, const void *dO, const int32_t *belo
  * Products are accumulated, and the state is kept, in fp32; bf16 outputs are
  * rounded once.  Accuracy versus the fp64 definition: 1e-5 (GA_F32 and every
  * state), 5e-3 (GA_BF16), each as the 2-norm of the error over the result's.
- * Every reduction has a fixed order: repeated calls give identical bits.
+ * Every reduction has a fixed order: repeated calls give identical bits.  (In
+ * GA_BF16 a call that hands a state back forms it to more bits than one that
+ * does not, so the two may differ in the last bits of their outputs.)
  * Pointer, stream and error conventions as above (4-byte alignment is enough
  * for log_decay and lengths); the workspace is ga_linear_workspace_bytes
  * (0: none needed, the pointer may then be NULL).  Outputs must not overlap

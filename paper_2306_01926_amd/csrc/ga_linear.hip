@@ -27,17 +27,30 @@ namespace {
 
 constexpr int kStep = 16;  // tokens staged at a time
 
-// One step's decay of a state value, l x.  Many steps in a row compound what l
-// is off by, and 2^-24 of an l near one is large against 1 - l; l - 1 is formed
-// without that loss, and l x as x + (l - 1) x with one rounding.  A small l is
-// exact enough as it is, and l - 1 would not be.
+// The decay of a state value over some tokens, l^n x.  Many decays in a row
+// compound what the factor is off by, and 2^-24 of a factor near one is large
+// against its distance to one; l^n - 1 is formed without that loss, and l^n x
+// as x + (l^n - 1) x.  A small factor is exact enough as it is, and l^n - 1
+// would not be.
 struct Decay {
-  float a, b;  // l = a + b with b 0 or 1
-  __device__ __forceinline__ explicit Decay(float log_decay) {
-    b = log_decay > -0.5f ? 1.f : 0.f;
-    a = b != 0.f ? expm1f(log_decay) : expf(log_decay);
+  float a, b;  // l^n = a + b with b 0 or 1
+  __device__ __forceinline__ explicit Decay(float log_decay_n) {
+    b = log_decay_n > -0.5f ? 1.f : 0.f;
+    a = b != 0.f ? expm1f(log_decay_n) : expf(log_decay_n);
   }
   __device__ __forceinline__ float operator()(float x) const { return fmaf(a, x, b * x); }
+};
+// The same for a walk's equal chunks as one factor each: what the rounding of
+// one is off by is taken from the next, so that their product is not.
+struct Decays {
+  Decay l;
+  float off;
+  __device__ __forceinline__ explicit Decays(float log_decay_n) : l(log_decay_n), off(0.f) {}
+  __device__ __forceinline__ float next() {
+    const float a = l.a + off, w = a + l.b;
+    off = a - (w - l.b);
+    return w;
+  }
 };
 
 __device__ __forceinline__ int length_of(const int32_t* lengths, int64_t b, int n) {
@@ -156,7 +169,8 @@ __global__ __launch_bounds__(256) void k_lin_heads(const float* __restrict__ par
 // Roundings: the scores after decay and the state that Q meets are rounded to
 // bf16, as the matrix cores need (each term of an output passes one of the
 // two); the state itself is fp32, and the decayed keys that it sums are kept
-// as two bf16 parts (16 significant bits), two products each.
+// as two bf16 parts (16 significant bits), two products each, or as three where
+// the state is handed back: two leave it off by 2e-6 of its 2-norm.
 constexpr int kC = 64;         // tokens per chunk
 constexpr int kTile = kC * 128;  // bytes of a chunk's rows of 64 bf16
 constexpr float kLog2e = 1.4426950408889634f;
@@ -230,7 +244,7 @@ struct Segment {
   const uint16_t *q, *k, *v, *w;
   int64_t bh;
   int p, len, c0, c1;
-  float g, ks;
+  float g, ld, ks;
 
   __device__ __forceinline__ Segment(const Chunked& A, int64_t slice, int segment) : bh(slice), p(segment) {
     const int h = (int)(bh % A.H);
@@ -240,6 +254,7 @@ struct Segment {
     k = A.k + (A.k_shared ? bk : bh) * A.n * 64;
     v = A.v + (A.v_shared ? bk : bh) * A.n * 64;
     w = A.w + (A.w_shared ? bk : bh) * A.n * 64;
+    ld = fmaxf(A.log_decay[h], -1.0e30f);
     g = decay_log2(A.log_decay[h]);
     ks = REV ? A.scale : 1.f;
     c0 = p * A.cps;
@@ -257,16 +272,26 @@ struct Segment {
     const int64_t t = (int64_t)A.cps * kC;
     return (float)min(max((int64_t)len - u * t, (int64_t)0), t);
   }
-  // granule x of row rr of chunk c, decayed to the chunk's end, in two bf16 parts
-  __device__ __forceinline__ void decayed(u32x4 x, int rr, int c, u32x4& hi, u32x4& lo) const {
+  // granule x of row rr of chunk c, decayed to the chunk's end, in bf16 parts
+  template <int PARTS>
+  __device__ __forceinline__ void decayed(u32x4 x, int rr, int c, u32x4 (&part)[PARTS]) const {
     // rows behind the end are zeros
     const float w = ks * decay_pow(g, (float)(max(count(c) - 1 - rr, 0) + REV));
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const float a = w * bf16_to_f32(x[e] & 0xffffu), b = w * __uint_as_float(x[e] & 0xffff0000u);
-      hi[e] = pack_bf16x2(a, b);
-      lo[e] = pack_bf16x2(a - bf16_to_f32(hi[e] & 0xffffu), b - __uint_as_float(hi[e] & 0xffff0000u));
+      float a = w * bf16_to_f32(x[e] & 0xffffu), b = w * __uint_as_float(x[e] & 0xffff0000u);
+#pragma unroll
+      for (int i = 0; i < PARTS; ++i) {
+        part[i][e] = pack_bf16x2(a, b);
+        a -= bf16_to_f32(part[i][e] & 0xffffu);
+        b -= __uint_as_float(part[i][e] & 0xffff0000u);
+      }
     }
+  }
+  // the state's decay over chunk c (all but the last are whole)
+  __device__ __forceinline__ float over(int c, Decays& whole) const {
+    const int nr = count(c);
+    return nr < kC ? decay_pow(g, (float)nr) : whole.next();
   }
   // Walks the segment's chunks: load(c, R) requests the rows of chunk c, three
   // chunks ahead of their use (HBM answers after about the time of two),
@@ -341,10 +366,38 @@ __device__ __forceinline__ void store_tokens(Buffer b, const Segment<REV>& G, in
   }
 }
 
+// A wave's operands for the update of its quadrant of the state (features 32 ah
+// of the keys, 32 ch of the values): the value tile's columns and those of the
+// decayed keys' parts, which lie behind each other.  Two chains of products run
+// side by side, the first parts' into S, the others' into T.
+template <int PARTS>
+struct StateUpdate {
+  u32x4 vf[4], kf[PARTS][4];  // step x contracts tokens 16 x + {4 hf + 0..3, 8 + 4 hf + 0..3}
+  __device__ __forceinline__ StateUpdate(const unsigned char* values, const unsigned char* keys, const Lanes& L, int ah,
+                                         int ch) {
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      const int ra = 16 * x + 4 * L.hf;
+      vf[x] = join(L.perm(values, ra, ch), L.perm(values, ra + 8, ch));
+#pragma unroll
+      for (int i = 0; i < PARTS; ++i)
+        kf[i][x] = join(L.nat(keys + i * kTile, ra, ah), L.nat(keys + i * kTile, ra + 8, ah));
+    }
+  }
+  __device__ __forceinline__ void add(f32x16& S, f32x16& T) const {
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      S = mfma(vf[x], kf[0][x], S);
+#pragma unroll
+      for (int i = 1; i < PARTS; ++i) T = mfma(vf[x], kf[i][x], T);
+    }
+  }
+};
+
 // The local states of the segments but the last, from zero: four waves, a
 // quadrant of the state each.
-template <bool REV>
-__device__ __forceinline__ void local_states(const Chunked& A, unsigned char (*lds)[3 * kTile]) {
+template <bool REV, int PARTS>
+__device__ __forceinline__ void local_states(const Chunked& A, unsigned char (*lds)[(1 + PARTS) * kTile]) {
   const int64_t bh = blockIdx.x / (A.P - 1);
   const Segment<REV> G(A, bh, (int)(blockIdx.x - bh * (A.P - 1)));
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -354,15 +407,16 @@ __device__ __forceinline__ void local_states(const Chunked& A, unsigned char (*l
     u32x4 k[2], v[2];
   };
   f32x16 S = zero16();
+  Decays whole(G.ld * kC);
   auto put = [&](int c, int buf, const Rows& R) __attribute__((always_inline)) {
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      u32x4 hi, lo;
-      G.decayed(R.k[u], r0 + 32 * u, c, hi, lo);
+      u32x4 part[PARTS];
+      G.decayed(R.k[u], r0 + 32 * u, c, part);
       const int at = toff(r0 + 32 * u, gr);
       *(u32x4*)(lds[buf] + at) = R.v[u];
-      *(u32x4*)(lds[buf] + kTile + at) = hi;
-      *(u32x4*)(lds[buf] + 2 * kTile + at) = lo;
+#pragma unroll
+      for (int i = 0; i < PARTS; ++i) *(u32x4*)(lds[buf] + (1 + i) * kTile + at) = part[i];
     }
   };
   G.template walk<Rows>(
@@ -379,24 +433,13 @@ __device__ __forceinline__ void local_states(const Chunked& A, unsigned char (*l
       put,
       [&](int c, int buf, const Rows& next) __attribute__((always_inline)) {
         const unsigned char* t = lds[buf];
-        const float w = decay_pow(G.g, (float)G.count(c));
-        u32x4 vf[4], kh[4], kl[4];  // step x contracts tokens 16 x + {4 hf + 0..3, 8 + 4 hf + 0..3}
-#pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          const int ra = 16 * x + 4 * L.hf;
-          vf[x] = join(L.perm(t, ra, ch), L.perm(t, ra + 8, ch));
-          kh[x] = join(L.nat(t + kTile, ra, ah), L.nat(t + kTile, ra + 8, ah));
-          kl[x] = join(L.nat(t + 2 * kTile, ra, ah), L.nat(t + 2 * kTile, ra + 8, ah));
-        }
+        const StateUpdate<PARTS> U(t, t + kTile, L, ah, ch);
         __builtin_amdgcn_sched_barrier(0);
+        const float w = G.over(c, whole);
 #pragma unroll
         for (int x = 0; x < 16; ++x) S[x] *= w;
         f32x16 T = zero16();
-#pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          S = mfma(vf[x], kh[x], S);
-          T = mfma(vf[x], kl[x], T);
-        }
+        U.add(S, T);
         put(c + 1, buf ^ 1, next);
 #pragma unroll
         for (int x = 0; x < 16; ++x) S[x] += T[x];
@@ -407,17 +450,19 @@ __device__ __forceinline__ void local_states(const Chunked& A, unsigned char (*l
 }
 
 // grid (slices (P - 1), directions): a gradient needs the states of both walks.
-__global__ __launch_bounds__(256, 3) void k_lin_states(Chunked F, Chunked B) {
-  __shared__ __attribute__((aligned(16))) unsigned char lds[2][3 * kTile];  // V, K hi, K lo (decayed)
+template <int PARTS>
+__global__ __launch_bounds__(256, PARTS == 2 ? 3 : 2) void k_lin_states(Chunked F, Chunked B) {
+  __shared__ __attribute__((aligned(16))) unsigned char lds[2][(1 + PARTS) * kTile];  // V, the decayed K's parts
   if (blockIdx.y == 0)
-    local_states<false>(F, lds);
+    local_states<false, PARTS>(F, lds);
   else
-    local_states<true>(B, lds);
+    local_states<true, PARTS>(B, lds);
 }
 
 // Outputs of a forward walk (and the final state): workgroup `block` of slices P.
-constexpr int kForwardBuf = 6 * kTile;  // K, K hi, K lo (decayed), V, the state, Q
-__device__ __forceinline__ void forward_walk(const Chunked& A, int block, unsigned char (*lds)[kForwardBuf]) {
+constexpr int forward_buf(int PARTS) { return (4 + PARTS) * kTile; }  // V, the state, Q, K, the decayed K's parts
+template <int PARTS>
+__device__ __forceinline__ void forward_walk(const Chunked& A, int block, unsigned char (*lds)[forward_buf(PARTS)]) {
   const int64_t bh = block / A.P;
   const Segment<false> G(A, bh, (int)(block - bh * A.P));
   // the wave's index is scalar, so that branches on it are jumps: matrix
@@ -425,14 +470,14 @@ __device__ __forceinline__ void forward_walk(const Chunked& A, int block, unsign
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lane = tid & 63;
   const Lanes L(lane);
-  constexpr int kV = 3 * kTile, kS = 4 * kTile, kQ = 5 * kTile;
+  constexpr int kV = 0, kS = kTile, kQ = 2 * kTile, kK = 3 * kTile;
   const int ch = (wave >> 1) & 1;
 
-  auto put_key = [&](int buf, int row, int gr, u32x4 k, u32x4 hi, u32x4 lo) __attribute__((always_inline)) {
-    const int at = toff(row, gr);
-    *(u32x4*)(lds[buf] + at) = k;
-    *(u32x4*)(lds[buf] + kTile + at) = hi;
-    *(u32x4*)(lds[buf] + 2 * kTile + at) = lo;
+  auto put_key = [&](int buf, int row, int gr, u32x4 k, const u32x4(&part)[PARTS]) __attribute__((always_inline)) {
+    unsigned char* t = lds[buf] + kK + toff(row, gr);
+    *(u32x4*)t = k;
+#pragma unroll
+    for (int i = 0; i < PARTS; ++i) *(u32x4*)(t + (1 + i) * kTile) = part[i];
   };
 
   if (wave >= 4) {
@@ -460,9 +505,10 @@ __device__ __forceinline__ void forward_walk(const Chunked& A, int block, unsign
         for (int x = 0; x < 16; ++x) S[x] = fmaf(w, S[x], s0[x]);
       }
     }
-    u32x4 hi, lo;
+    u32x4 part[PARTS];
+    Decays whole(G.ld * kC);
     auto put = [&](int buf, const Rows& R) __attribute__((always_inline)) {
-      put_key(buf, r0, gr, R.k, hi, lo);
+      put_key(buf, r0, gr, R.k, part);
 #pragma unroll
       for (int u = 0; u < 2; ++u) *(u32x4*)(lds[buf] + kV + toff(r0 + 32 * u, gr)) = R.v[u];
     };
@@ -482,37 +528,26 @@ __device__ __forceinline__ void forward_walk(const Chunked& A, int block, unsign
           for (int u = 0; u < 2; ++u) R.v[u] = buf_load(bv, G.place(r0 + 32 * u, nr) * 128 + 16 * gr);
         },
         [&](int c, int buf, const Rows& R) __attribute__((always_inline)) {
-          G.decayed(R.k, r0, c, hi, lo);
+          G.decayed(R.k, r0, c, part);
           put(buf, R);
           put_state(buf);
         },
         [&](int c, int buf, const Rows& next) __attribute__((always_inline)) {
           const unsigned char* t = lds[buf];
-          const float w = decay_pow(G.g, (float)G.count(c));
           // the conversion comes first: the output's waves have the LDS then
-          G.decayed(next.k, r0, c + 1, hi, lo);
+          G.decayed(next.k, r0, c + 1, part);
+          const float w = G.over(c, whole);
 #pragma unroll
           for (int x = 0; x < 16; ++x) S[x] *= w;
-          __builtin_amdgcn_sched_barrier(0);
-          u32x4 vf[4], kh[4], kl[4];  // step x contracts tokens 16 x + {4 hf + 0..3, 8 + 4 hf + 0..3}
-#pragma unroll
-          for (int x = 0; x < 4; ++x) {
-            const int ra = 16 * x + 4 * L.hf;
-            vf[x] = join(L.perm(t + kV, ra, ch), L.perm(t + kV, ra + 8, ch));
-            kh[x] = join(L.nat(t + kTile, ra, ah), L.nat(t + kTile, ra + 8, ah));
-            kl[x] = join(L.nat(t + 2 * kTile, ra, ah), L.nat(t + 2 * kTile, ra + 8, ah));
-          }
           f32x16 T = zero16();
+          __builtin_amdgcn_sched_barrier(0);
+          const StateUpdate<PARTS> U(t + kV, t + kK + kTile, L, ah, ch);
+          U.add(S, T);
+          __builtin_amdgcn_sched_group_barrier(0x100, 8 + 4 * PARTS - 4, 0);
 #pragma unroll
           for (int x = 0; x < 4; ++x) {
-            S = mfma(vf[x], kh[x], S);
-            T = mfma(vf[x], kl[x], T);
-          }
-          __builtin_amdgcn_sched_group_barrier(0x100, 12, 0);
-#pragma unroll
-          for (int x = 0; x < 4; ++x) {
-            __builtin_amdgcn_sched_group_barrier(0x8, 2, 0);
-            if (x < 2) __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
+            __builtin_amdgcn_sched_group_barrier(0x8, PARTS, 0);
+            if (x < 2) __builtin_amdgcn_sched_group_barrier(0x100, 2 + 2 * PARTS, 0);
           }
           __builtin_amdgcn_sched_barrier(0);
           put(buf ^ 1, next);
@@ -546,18 +581,18 @@ __device__ __forceinline__ void forward_walk(const Chunked& A, int block, unsign
       struct Rows {
         u32x4 x[kRows];
       };
-      u32x4 hi[2], lo[2];
+      u32x4 part[2][PARTS];
       auto convert = [&](int c, const Rows& R) __attribute__((always_inline)) {
         if constexpr (RB == 0) {
 #pragma unroll
-          for (int u = 0; u < 2; ++u) G.decayed(R.x[u], 32 + r0 + 16 * u, c, hi[u], lo[u]);
+          for (int u = 0; u < 2; ++u) G.decayed(R.x[u], 32 + r0 + 16 * u, c, part[u]);
         }
       };
       auto put = [&](int buf, const Rows& R) __attribute__((always_inline)) {
 #pragma unroll
         for (int u = 0; u < kRows; ++u) {
           if constexpr (RB == 0)
-            put_key(buf, 32 + r0 + 16 * u, gr, R.x[u], hi[u], lo[u]);
+            put_key(buf, 32 + r0 + 16 * u, gr, R.x[u], part[u]);
           else
             *(u32x4*)(lds[buf] + kQ + toff(r0 + 16 * u, gr)) = R.x[u];
         }
@@ -582,7 +617,7 @@ __device__ __forceinline__ void forward_walk(const Chunked& A, int block, unsign
 #pragma unroll
             for (int s = 0; s < 4; ++s)
 #pragma unroll
-              for (int kb = 0; kb <= RB; ++kb) kf[kb][s] = *(const u32x4*)(t + toff(32 * kb + L.r, 2 * s + L.hf));
+              for (int kb = 0; kb <= RB; ++kb) kf[kb][s] = *(const u32x4*)(t + kK + toff(32 * kb + L.r, 2 * s + L.hf));
 #pragma unroll
             for (int s = 0; s < 4; ++s)
               sf[s] = join(L.perm(t + kS, 16 * s + 8 * L.hf, ch), L.perm(t + kS, 16 * s + 8 * L.hf + 4, ch));
@@ -642,10 +677,10 @@ __device__ __forceinline__ void forward_walk(const Chunked& A, int block, unsign
 // Eight waves: waves 0-3 form 32 tokens by 64 features of dV (0, 1) or dK
 // (2, 3), waves 4-7 the state.  out: dV, out2: dK; OUT32: they are fp32 (a
 // query head's share of a shared head's gradient).
-constexpr int kBackwardBuf = 7 * kTile;  // Q, Q hi, Q lo (decayed), dO, K, V, the state
-template <bool OUT32>
-__device__ __forceinline__ void backward_walk(const Chunked& A, int block, unsigned char (*lds)[kBackwardBuf]) {
-  constexpr int kQ = 0, kO = 3 * kTile, kK = 4 * kTile, kV = 5 * kTile, kS = 6 * kTile;
+constexpr int backward_buf(int PARTS) { return (5 + PARTS) * kTile; }  // dO, K, V, the state, Q, the decayed Q's parts
+template <bool OUT32, int PARTS>
+__device__ __forceinline__ void backward_walk(const Chunked& A, int block, unsigned char (*lds)[backward_buf(PARTS)]) {
+  constexpr int kO = 0, kK = kTile, kV = 2 * kTile, kS = 3 * kTile, kQ = 4 * kTile;
   const int64_t bh = block / A.P;
   const Segment<true> G(A, bh, (int)(block - bh * A.P));
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -657,7 +692,7 @@ __device__ __forceinline__ void backward_walk(const Chunked& A, int block, unsig
     u32x4 k, v, q, w;
   };
   const int gr = tid & 7, r0 = tid >> 3, at = toff(r0, gr);
-  u32x4 hi, lo;
+  u32x4 part[PARTS];
   auto load = [&](int c, Rows& R) __attribute__((always_inline)) {
     const int nr = G.count(c);
     const int64_t f = G.first(c, nr) * 64;
@@ -670,8 +705,8 @@ __device__ __forceinline__ void backward_walk(const Chunked& A, int block, unsig
   auto put = [&](int buf, const Rows& R) __attribute__((always_inline)) {
     unsigned char* t = lds[buf] + at;
     *(u32x4*)(t + kQ) = R.k;
-    *(u32x4*)(t + kQ + kTile) = hi;
-    *(u32x4*)(t + kQ + 2 * kTile) = lo;
+#pragma unroll
+    for (int i = 0; i < PARTS; ++i) *(u32x4*)(t + kQ + (1 + i) * kTile) = part[i];
     *(u32x4*)(t + kO) = R.v;
     *(u32x4*)(t + kK) = R.q;
     *(u32x4*)(t + kV) = R.w;
@@ -680,6 +715,7 @@ __device__ __forceinline__ void backward_walk(const Chunked& A, int block, unsig
   if (wave >= 4) {
     const int ah = wave & 1, ch = (wave >> 1) & 1, sa = 32 * ah + L.r, sc = 32 * ch + 16 * L.hf;
     f32x16 S = zero16();
+    Decays whole(G.ld * kC);
     const float* s0 = A.scanned ? A.seg + (bh * A.P + G.p) * 4096 : (A.state ? A.state + bh * 4096 : nullptr);
     if (s0) {
 #pragma unroll
@@ -703,31 +739,20 @@ __device__ __forceinline__ void backward_walk(const Chunked& A, int block, unsig
     G.template walk<Rows>(
         load,
         [&](int c, int buf, const Rows& R) __attribute__((always_inline)) {
-          G.decayed(R.k, r0, c, hi, lo);
+          G.decayed(R.k, r0, c, part);
           put(buf, R);
           put_state(buf);
         },
         [&](int c, int buf, const Rows& next) __attribute__((always_inline)) {
           const unsigned char* t = lds[buf];
-          const float w = decay_pow(G.g, (float)G.count(c));
-          G.decayed(next.k, r0, c + 1, hi, lo);
+          G.decayed(next.k, r0, c + 1, part);
+          const float w = G.over(c, whole);
 #pragma unroll
           for (int x = 0; x < 16; ++x) S[x] *= w;
-          __builtin_amdgcn_sched_barrier(0);
-          u32x4 vf[4], kh[4], kl[4];
-#pragma unroll
-          for (int x = 0; x < 4; ++x) {
-            const int ra = 16 * x + 4 * L.hf;
-            vf[x] = join(L.perm(t + kO, ra, ch), L.perm(t + kO, ra + 8, ch));
-            kh[x] = join(L.nat(t + kQ + kTile, ra, ah), L.nat(t + kQ + kTile, ra + 8, ah));
-            kl[x] = join(L.nat(t + kQ + 2 * kTile, ra, ah), L.nat(t + kQ + 2 * kTile, ra + 8, ah));
-          }
           f32x16 T = zero16();
-#pragma unroll
-          for (int x = 0; x < 4; ++x) {
-            S = mfma(vf[x], kh[x], S);
-            T = mfma(vf[x], kl[x], T);
-          }
+          __builtin_amdgcn_sched_barrier(0);
+          const StateUpdate<PARTS> U(t + kO, t + kQ + kTile, L, ah, ch);
+          U.add(S, T);
           put(buf ^ 1, next);
 #pragma unroll
           for (int x = 0; x < 16; ++x) S[x] += T[x];
@@ -758,7 +783,7 @@ __device__ __forceinline__ void backward_walk(const Chunked& A, int block, unsig
       G.template walk<Rows>(
           load,
           [&](int c, int buf, const Rows& R) __attribute__((always_inline)) {
-            G.decayed(R.k, r0, c, hi, lo);
+            G.decayed(R.k, r0, c, part);
             put(buf, R);
           },
           [&](int c, int buf, const Rows& next) __attribute__((always_inline)) {
@@ -788,7 +813,7 @@ __device__ __forceinline__ void backward_walk(const Chunked& A, int block, unsig
                   o[e] = mfma(join(L.perm(t + kS, 16 * s + 8 * L.hf, e), L.perm(t + kS, 16 * s + 8 * L.hf + 4, e)),
                               qf[s], o[e]);
             }
-            G.decayed(next.k, r0, c + 1, hi, lo);
+            G.decayed(next.k, r0, c + 1, part);
 #pragma unroll
             for (int u = 0; u < 2 * RB + 2; ++u)
 #pragma unroll
@@ -826,22 +851,25 @@ __device__ __forceinline__ void backward_walk(const Chunked& A, int block, unsig
   }
 }
 
-// grid: slices P.
+// grid: slices P.  PARTS: 3 where the final state is handed back.
+template <int PARTS>
 __global__ __launch_bounds__(512, 2) void k_lin_forward(Chunked A) {
-  __shared__ __attribute__((aligned(16))) unsigned char lds[2][kForwardBuf];
-  forward_walk(A, blockIdx.x, lds);
+  __shared__ __attribute__((aligned(16))) unsigned char lds[2][forward_buf(PARTS)];
+  forward_walk<PARTS>(A, blockIdx.x, lds);
 }
 
 // dQ (the forward walk F) and dK, dV (the backward walk B) side by side: they
 // share no result, and one launch of both fills the compute units where one of
 // them would not.  grid: slices (B.P + F.P), the longer backward walks first.
-template <bool OUT32>
+// PARTS: 3 where the initial state's gradient is handed back.
+template <bool OUT32, int PARTS>
 __global__ __launch_bounds__(512, 2) void k_lin_backward(Chunked F, Chunked B, int backward) {
-  __shared__ __attribute__((aligned(16))) unsigned char lds[2 * kBackwardBuf];
+  __shared__ __attribute__((aligned(16))) unsigned char lds[2 * backward_buf(PARTS)];
+  static_assert(forward_buf(2) <= backward_buf(PARTS), "the forward walk's tiles fit");
   if ((int)blockIdx.x < backward)
-    backward_walk<OUT32>(B, blockIdx.x, (unsigned char(*)[kBackwardBuf])lds);
+    backward_walk<OUT32, PARTS>(B, blockIdx.x, (unsigned char(*)[backward_buf(PARTS)])lds);
   else
-    forward_walk(F, blockIdx.x - backward, (unsigned char(*)[kForwardBuf])lds);
+    forward_walk<2>(F, blockIdx.x - backward, (unsigned char(*)[forward_buf(2)])lds);
 }
 
 // Local states of the segments to the states before them, in place:
@@ -859,7 +887,8 @@ __global__ __launch_bounds__(256) void k_lin_scan(Scan F, Scan B) {
   if (!A.wanted) return;
   const int64_t bh = blockIdx.x >> 4;
   const int e = (blockIdx.x & 15) * 256 + threadIdx.x;
-  const float g = decay_log2(A.log_decay[bh % A.H]);
+  const float ld = fmaxf(A.log_decay[bh % A.H], -1.0e30f);
+  const Decay whole(ld * A.tokens);
   const int len = length_of(A.lengths, bh / A.H, A.n);
   float s = !A.state ? 0.f : A.state[bh * 4096 + (A.transposed ? (e & 63) * 64 + (e >> 6) : e)];
   float* at = A.seg + bh * A.P * 4096 + e;
@@ -872,7 +901,7 @@ __global__ __launch_bounds__(256) void k_lin_scan(Scan F, Scan B) {
       if (p0 + u >= A.P) break;
       at[(int64_t)(p0 + u) * 4096] = s;
       const int64_t tokens = min(max((int64_t)len - (int64_t)(p0 + u) * A.tokens, (int64_t)0), (int64_t)A.tokens);
-      s = fmaf(decay_pow(g, (float)tokens), s, local[u]);
+      s = (tokens == A.tokens ? whole : Decay(ld * tokens))(s) + local[u];
     }
   }
 }
@@ -936,6 +965,7 @@ __device__ __forceinline__ void walk32(const Walk32& A, int block, int items, fl
   float* out = A.out + bh * A.n * 64 + 32 * ch;
   const float g = decay_log2(A.log_decay[h]);
   const float ks = REV ? A.scale : 1.f;
+  Decays whole(fmaxf(A.log_decay[h], -1.0e30f) * kC32);
   const int64_t t0 = (int64_t)p * A.tokens, t1 = min(t0 + A.tokens, (int64_t)len);
   auto jx = [&](int x) __attribute__((always_inline)) { return 8 * (x / 4) + 4 * hf + x % 4; };
 
@@ -1025,7 +1055,7 @@ __device__ __forceinline__ void walk32(const Walk32& A, int block, int items, fl
       }
       __builtin_amdgcn_sched_barrier(0);
     }
-    const float w = decay_pow(g, (float)nr);
+    const float w = nr < kC32 ? decay_pow(g, (float)nr) : whole.next();
 #pragma unroll
     for (int e = 0; e < 2; ++e)
 #pragma unroll
@@ -1105,11 +1135,17 @@ void set_split(Chunked& a, Split s) {
 }
 
 // The states before the segments of one walk, or of the two of a gradient.
-void segment_states(const LinearDims& d, const Chunked& f, const Chunked& b, unsigned directions, hipStream_t st) {
+// exact: a state is handed back.
+void segment_states(const LinearDims& d, const Chunked& f, const Chunked& b, unsigned directions, bool exact,
+                    hipStream_t st) {
   const unsigned slices = (unsigned)(d.B * d.H);
   if (f.P > 1) {
     TimedLaunch tl("lin_states", st);
-    hipLaunchKernelGGL(k_lin_states, dim3(slices * (f.P - 1), directions), dim3(256), 0, st, f, b);
+    const dim3 grid(slices * (f.P - 1), directions);
+    if (exact)
+      hipLaunchKernelGGL(k_lin_states<3>, grid, dim3(256), 0, st, f, b);
+    else
+      hipLaunchKernelGGL(k_lin_states<2>, grid, dim3(256), 0, st, f, b);
   }
   if (f.scanned || b.scanned) {
     TimedLaunch tl("lin_scan", st);
@@ -1172,9 +1208,13 @@ hipError_t launch_linear(const LinearDims& d, const void* Q, const void* K, cons
     a.seg = (float*)ws, a.state_out = state_out, a.out = O;
     a.H = d.H, a.Hk = d.Hk, a.n = d.n, a.scale = scale;
     set_split(a, split_of(d, 1));
-    segment_states(d, a, Chunked{}, 1, st);
+    segment_states(d, a, Chunked{}, 1, state_out != nullptr, st);
     TimedLaunch tl("lin_forward", st);
-    hipLaunchKernelGGL(k_lin_forward, dim3((unsigned)(d.B * d.H * a.P)), dim3(512), 0, st, a);
+    const dim3 wgs((unsigned)(d.B * d.H * a.P));
+    if (state_out)
+      hipLaunchKernelGGL(k_lin_forward<3>, wgs, dim3(512), 0, st, a);
+    else
+      hipLaunchKernelGGL(k_lin_forward<2>, wgs, dim3(512), 0, st, a);
     return hipGetLastError();
   }
   Walk32 a = walk32_of(d, split32_of(d, 1), log_decay, lengths, scale);
@@ -1227,15 +1267,21 @@ hipError_t launch_linear_grad(const LinearDims& d, const void* Q, const void* K,
     b.seg = a.seg + seg_bytes(d, s) / 4;
     set_split(a, s);
     set_split(b, s);
-    segment_states(d, a, b, 2, st);
+    segment_states(d, a, b, 2, dstate_out != nullptr, st);
     {
       TimedLaunch tl("lin_backward", st);
       const int half = d.B * d.H * s.P;
       const dim3 wgs((unsigned)(2 * half));
-      if (grouped)
-        hipLaunchKernelGGL(k_lin_backward<true>, wgs, dim3(512), 0, st, a, b, half);
-      else
-        hipLaunchKernelGGL(k_lin_backward<false>, wgs, dim3(512), 0, st, a, b, half);
+#define GA_LIN_BACKWARD(OUT32, PARTS) \
+  hipLaunchKernelGGL((k_lin_backward<OUT32, PARTS>), wgs, dim3(512), 0, st, a, b, half)
+      if (dstate_out) {
+        if (grouped) GA_LIN_BACKWARD(true, 3);
+        else GA_LIN_BACKWARD(false, 3);
+      } else {
+        if (grouped) GA_LIN_BACKWARD(true, 2);
+        else GA_LIN_BACKWARD(false, 2);
+      }
+#undef GA_LIN_BACKWARD
     }
     heads(b.out, dV);
     heads(b.out2, dK);
