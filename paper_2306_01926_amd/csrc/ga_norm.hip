@@ -80,34 +80,36 @@ struct Eight {
       }
     }
   }
-  __device__ __forceinline__ void get(float (&v)[kE]) const {
-    constexpr int kN = 4 * kWords;
-    uint32_t x[kN];
-#pragma unroll
-    for (int i = 0; i < kN; ++i) x[i] = w[i];
+  // shifts the group into place, before get: few lanes need it, and a wave with
+  // none of them jumps over it
+  __device__ __forceinline__ void settle() {
     if constexpr (!VEC) {
+      constexpr int kN = 4 * kWords;
+      if (!__any(behind != 0)) return;
 #pragma unroll
       for (int s = kE; s >= 1; s /= 2) {  // by 8, 4, 2 and 1 features
         const bool on = (behind & s) != 0;
 #pragma unroll
         for (int i = 0; i < kN; ++i) {
+          uint32_t y;
           if constexpr (DT::kBits == 16) {
-            const uint32_t hi = i + 1 < kN ? x[i + 1] : 0u;
-            const uint32_t y = s == 1 ? x[i] >> 16 | hi << 16 : (i + s / 2 < kN ? x[i + s / 2 < kN ? i + s / 2 : 0] : 0u);
-            x[i] = on ? y : x[i];
+            const uint32_t hi = i + 1 < kN ? w[i + 1 < kN ? i + 1 : 0] : 0u;
+            y = s == 1 ? w[i] >> 16 | hi << 16 : (i + s / 2 < kN ? w[i + s / 2 < kN ? i + s / 2 : 0] : 0u);
           } else {
-            const uint32_t y = i + s < kN ? x[i + s < kN ? i + s : 0] : 0u;
-            x[i] = on ? y : x[i];
+            y = i + s < kN ? w[i + s < kN ? i + s : 0] : 0u;
           }
+          w[i] = on ? y : w[i];
         }
       }
     }
+  }
+  __device__ __forceinline__ void get(float (&v)[kE]) const {
 #pragma unroll
     for (int e = 0; e < kE; ++e) {
       if constexpr (DT::kBits == 16)
-        v[e] = __uint_as_float(e & 1 ? x[e / 2] & 0xffff0000u : x[e / 2] << 16);
+        v[e] = __uint_as_float(e & 1 ? w[e / 2] & 0xffff0000u : w[e / 2] << 16);
       else
-        v[e] = __uint_as_float(x[e]);
+        v[e] = __uint_as_float(w[e]);
     }
   }
 
@@ -129,6 +131,7 @@ template <class DT, bool VEC>
 __device__ __forceinline__ void load8(const typename DT::T* p, int c, int W, float (&v)[kE]) {
   Eight<DT, VEC> x;
   x.load(p, c, W);
+  x.settle();
   x.get(v);
 }
 
@@ -282,9 +285,9 @@ __global__ __launch_bounds__(wg_threads(TPR)) void k_norm(NormArgs<DT> A, typena
     const bool live = row0 + team < A.rows;
     const int64_t row = min(row0 + team, A.rows - 1);
     float y[kE], u[kE];
-    nx.get(y);
-    if (A.F) nf.get(u);
-    if (A.gate_batches > 1) ng.get(gt);
+    nx.settle(), nx.get(y);
+    if (A.F) nf.settle(), nf.get(u);
+    if (A.gate_batches > 1) ng.settle(), ng.get(gt);
     request(row0 + step);
 #pragma unroll
     for (int e = 0; e < kE; ++e) y[e] *= A.a;
@@ -316,9 +319,34 @@ struct NormParts {
   int64_t group_rows;
 };
 
+// A thread's sums of one parameter's gradient over the rows, in registers or in
+// LDS.
+template <bool LDS>
+struct Sums {
+  float v[LDS ? 1 : kE];
+  float* at;
+  __device__ __forceinline__ void start(float* lds) {
+    at = lds + threadIdx.x;
+#pragma unroll
+    for (int e = 0; e < kE; ++e) (LDS ? at[1024 * e] : v[LDS ? 0 : e]) = 0.f;
+  }
+  __device__ __forceinline__ void add(int e, float a, float b) {
+    float& s = LDS ? at[1024 * e] : v[LDS ? 0 : e];
+    s = fmaf(a, b, s);
+  }
+  __device__ __forceinline__ void get(float (&x)[kE]) const {
+#pragma unroll
+    for (int e = 0; e < kE; ++e) x[e] = LDS ? at[1024 * e] : v[LDS ? 0 : e];
+  }
+};
+
 template <int TPR>
 __device__ __forceinline__ void team_store(const float (&v)[kE], float* buf, float* dst, int W) {
   constexpr int kT = wg_threads(TPR), kTeams = kT / TPR;
+  if (kTeams == 1) {
+    store8<F32, false>(dst, threadIdx.x * kE, W, v);
+    return;
+  }
   __syncthreads();
 #pragma unroll
   for (int e = 0; e < kE; ++e) buf[(threadIdx.x / TPR) * (TPR * kE) + (threadIdx.x % TPR) * kE + e] = v[e];
@@ -332,6 +360,10 @@ __device__ __forceinline__ void team_store(const float (&v)[kE], float* buf, flo
 }
 
 // BIAS: the gradients of the norms' biases are asked for.
+// Threads of a team of 1024 have 128 registers each: they keep the sums in LDS,
+// read the parameters again (from the caches) where they use them and the rows
+// where they begin them (D = 8192, 4000 rows, bf16: 131 us, and 279 with all of
+// it in registers, most of them spilled).
 template <class DT, int TPR, bool VEC, bool BIAS>
 __global__ __launch_bounds__(wg_threads(TPR)) void k_norm_grad(NormArgs<DT> A, const typename DT::T* __restrict__ dY,
                                                                const typename DT::T* __restrict__ dH,
@@ -340,15 +372,24 @@ __global__ __launch_bounds__(wg_threads(TPR)) void k_norm_grad(NormArgs<DT> A, c
   constexpr int kT = wg_threads(TPR), kTeams = kT / TPR;
   using Raw = Eight<DT, VEC>;
   __shared__ float2 reds[2][6][16];
-  __shared__ float buf[kT * kE];
+  __shared__ float buf[kTeams > 1 ? kT * kE : 1];
   const int team = threadIdx.x / TPR, c = (threadIdx.x % TPR) * kE, W = A.W;
+  constexpr bool kLds = TPR == 1024;
   Raw pw, pb, gt, qw;  // (as stored: half the registers)
-  if (A.post_w) pw.load(A.post_w, c, W);
-  if (A.post_b) pb.load(A.post_b, c, W);
-  if (dH) qw.load(A.pre_w, c, W);
-  float spw[kE], sqw[kE], sg[kE], spb[kE], sqb[kE];
-#pragma unroll
-  for (int e = 0; e < kE; ++e) spw[e] = spb[e] = sqw[e] = sqb[e] = 0.f;
+  auto fetch = [&](Raw& r, const typename DT::T* p) __attribute__((always_inline)) { r.load(p, c, W), r.settle(); };
+  auto param = [&](Raw& r, const typename DT::T* p, float(&v)[kE]) __attribute__((always_inline)) {
+    if (kLds) fetch(r, p);
+    r.get(v);
+  };
+  if (!kLds && A.post_w) fetch(pw, A.post_w);
+  if (!kLds && A.post_b) fetch(pb, A.post_b);
+  if (!kLds && dH) fetch(qw, A.pre_w);
+  constexpr int kSums = kLds ? kT * kE : 0;
+  __shared__ float lds[kLds ? 4 * kSums : 1];
+  Sums<kLds> spw, sqw, spb, sqb;
+  spw.start(lds), sqw.start(lds + kSums);
+  if (BIAS) spb.start(lds + 2 * kSums), sqb.start(lds + 3 * kSums);
+  float sg[kE];
 
   int parity = 0;
   for (int i = 0; i < P.each; ++i) {
@@ -357,7 +398,8 @@ __global__ __launch_bounds__(wg_threads(TPR)) void k_norm_grad(NormArgs<DT> A, c
     const int share = P.split > 1 ? blockIdx.x % P.split : 0;
 #pragma unroll
     for (int e = 0; e < kE; ++e) sg[e] = 0.f;
-    if (A.gate_batches) gt.load(A.gate + (A.gate_batches > 1 ? (int64_t)grp * W : 0), c, W);
+    const typename DT::T* gate = A.gate_batches ? A.gate + (A.gate_batches > 1 ? (int64_t)grp * W : 0) : nullptr;
+    if (!kLds && gate) fetch(gt, gate);
     Raw nx, nf, ny, nh;  // the next row
     auto request = [&](int64_t r0) __attribute__((always_inline)) {
       const int64_t at = (grp * P.group_rows + min(r0 + team, P.group_rows - 1)) * W;
@@ -366,32 +408,33 @@ __global__ __launch_bounds__(wg_threads(TPR)) void k_norm_grad(NormArgs<DT> A, c
       if (dY) ny.load(dY + at, c, W);
       if (dH) nh.load(dH + at, c, W);
     };
-    request((int64_t)share * kTeams);
+    if (!kLds) request((int64_t)share * kTeams);
     for (int64_t r0 = (int64_t)share * kTeams; r0 < P.group_rows; r0 += (int64_t)P.split * kTeams) {
       float2(*red)[16] = reds[parity];
       parity ^= 1;
       // a team behind the last row works on it again, and its sums count nothing
       const float live = r0 + team < P.group_rows ? 1.f : 0.f;
       const int64_t row = grp * P.group_rows + min(r0 + team, P.group_rows - 1);
+      if (kLds) request(r0);
       float y[kE], fn[kE], d[kE], dh[kE], w[kE], g[kE], rf = 0.f;
-      nx.get(y);
-      if (A.F) nf.get(fn);
+      nx.settle(), nx.get(y);
+      if (A.F) nf.settle(), nf.get(fn);
       if (dY) {
-        ny.get(d);
+        ny.settle(), ny.get(d);
       } else {
 #pragma unroll
         for (int e = 0; e < kE; ++e) d[e] = 0.f;
       }
-      if (dH) nh.get(dh);
-      request(r0 + (int64_t)P.split * kTeams);
+      if (dH) nh.settle(), nh.get(dh);
+      if (!kLds) request(r0 + (int64_t)P.split * kTeams);
 #pragma unroll
       for (int e = 0; e < kE; ++e) y[e] *= A.a;
       // u = w fn + c, formed where it is used
       auto branch = [&](float(&u)[kE]) __attribute__((always_inline)) {
         if (A.post_w) {
-          pw.get(u);
+          param(pw, A.post_w, u);
           float s[kE];
-          if (A.post_b) pb.get(s);
+          if (A.post_b) param(pb, A.post_b, s);
 #pragma unroll
           for (int e = 0; e < kE; ++e) u[e] = fmaf(fn[e], u[e], A.post_b ? s[e] : 0.f);
         } else {
@@ -400,9 +443,9 @@ __global__ __launch_bounds__(wg_threads(TPR)) void k_norm_grad(NormArgs<DT> A, c
         }
       };
       auto gates = [&]() __attribute__((always_inline)) {
-        if (A.gate_batches) gt.get(g);
+        if (gate) param(gt, gate, g);
 #pragma unroll
-        for (int e = 0; e < kE; ++e) g[e] = A.gate_batches ? A.b * g[e] : A.b;
+        for (int e = 0; e < kE; ++e) g[e] = gate ? A.b * g[e] : A.b;
       };
       if (A.F) {
         if (A.post_w) rf = normalise<TPR>(fn, c, W, A.invW, A.layer, A.eps, red);
@@ -414,7 +457,7 @@ __global__ __launch_bounds__(wg_threads(TPR)) void k_norm_grad(NormArgs<DT> A, c
       if (dH) {
         // the sums that the projection needs go with those of the norm
         float sd = 0.f;
-        qw.get(w);
+        param(qw, A.pre_w, w);
 #pragma unroll
         for (int e = 0; e < kE; ++e) {
           w[e] *= dh[e];  // (zeros beyond W)
@@ -442,8 +485,8 @@ __global__ __launch_bounds__(wg_threads(TPR)) void k_norm_grad(NormArgs<DT> A, c
         for (int e = 0; e < kE; ++e) {
           y[e] *= rh;
           dh[e] *= live;
-          sqw[e] = fmaf(dh[e], y[e], sqw[e]);
-          if (BIAS) sqb[e] += dh[e];
+          sqw.add(e, dh[e], y[e]);
+          if (BIAS) sqb.add(e, 1.f, dh[e]);
         }
         project(w, y, rh, rh * m.y * A.invW, md, c, W);
 #pragma unroll
@@ -459,12 +502,12 @@ __global__ __launch_bounds__(wg_threads(TPR)) void k_norm_grad(NormArgs<DT> A, c
           du[e] = g[e] * d[e];
         }
         if (A.post_w) {
-          pw.get(w);
+          param(pw, A.post_w, w);
           float s = 0.f, sd = 0.f;
 #pragma unroll
           for (int e = 0; e < kE; ++e) {
-            spw[e] = fmaf(live * du[e], fn[e], spw[e]);
-            if (BIAS) spb[e] = fmaf(live, du[e], spb[e]);
+            spw.add(e, live * du[e], fn[e]);
+            if (BIAS) spb.add(e, live, du[e]);
             du[e] = c + e < W ? du[e] * w[e] : 0.f;
             s = fmaf(du[e], fn[e], s);
             sd += du[e];
@@ -484,13 +527,18 @@ __global__ __launch_bounds__(wg_threads(TPR)) void k_norm_grad(NormArgs<DT> A, c
   }
   if (P.part) {
     float* dst = P.part + (int64_t)blockIdx.x * 4 * W;
+    auto store = [&](const Sums<kLds>& s, int which) __attribute__((always_inline)) {
+      float v[kE];
+      s.get(v);
+      team_store<TPR>(v, buf, dst + (int64_t)which * W, W);
+    };
     if (A.post_w) {
-      team_store<TPR>(spw, buf, dst, W);
-      if (BIAS) team_store<TPR>(spb, buf, dst + W, W);
+      store(spw, 0);
+      if (BIAS) store(spb, 1);
     }
     if (dH) {
-      team_store<TPR>(sqw, buf, dst + 2 * W, W);
-      if (BIAS) team_store<TPR>(sqb, buf, dst + 3 * W, W);
+      store(sqw, 2);
+      if (BIAS) store(sqb, 3);
     }
   }
 }
