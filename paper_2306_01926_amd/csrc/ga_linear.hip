@@ -14,6 +14,7 @@
 #include <hip/hip_runtime.h>
 
 #include <float.h>
+#include <math.h>
 #include <stdint.h>
 
 #include <type_traits>
@@ -248,7 +249,7 @@ template <bool REV>
 struct Segment {
   const uint16_t *q, *k, *v, *w;
   int64_t bh;
-  int p, len, c0, c1;
+  int p, len, c0, c1, end;  // its chunks; where the walk ends
   float g, ld, ks;
 
   __device__ __forceinline__ Segment(const Chunked& A, int64_t slice, int segment) : bh(slice), p(segment) {
@@ -263,7 +264,7 @@ struct Segment {
     g = decay_log2(A.log_decay[h]);
     ks = REV ? A.scale : 1.f;
     c0 = p * A.cps;
-    c1 = min(c0 + A.cps, (len + kC - 1) / kC);
+    c1 = end = min(c0 + A.cps, (len + kC - 1) / kC);
   }
   // rows of chunk c (none behind the segment), the first one in memory, and
   // the place of walk row x among them (beyond them: out of the buffer)
@@ -306,7 +307,7 @@ struct Segment {
   // between them, which would cost copies of rows in flight (a wait for them).
   template <class Rows, class Load, class Put, class Step>
   __device__ __forceinline__ void walk(Load load, Put put, Step step) const {
-    if (c0 >= c1) return;
+    if (c0 >= end) return;
     Rows R0, R1, R2;
     load(c0, R0);
     load(c0 + 1, R1);
@@ -319,13 +320,13 @@ struct Segment {
       __syncthreads();
     };
     int c = c0, buf = 0;
-    for (; c + 3 <= c1; c += 3, buf ^= 1) {
+    for (; c + 3 <= end; c += 3, buf ^= 1) {
       turn(c, buf, R1, R0);
       turn(c + 1, buf ^ 1, R2, R1);
       turn(c + 2, buf, R0, R2);
     }
-    if (c < c1) turn(c, buf, R1, R0);
-    if (c + 1 < c1) turn(c + 1, buf ^ 1, R2, R1);
+    if (c < end) turn(c, buf, R1, R0);
+    if (c + 1 < end) turn(c + 1, buf ^ 1, R2, R1);
   }
 };
 
@@ -400,12 +401,24 @@ struct StateUpdate {
 };
 
 // The local states of the segments but the last, from zero: four waves, a
-// quadrant of the state each.
+// quadrant of the state each, walk the first half of a segment's chunks, four
+// more the second, and take the first half's state into theirs (one wave a SIMD
+// waits for its own LDS reads and products).
 template <bool REV, int PARTS>
-__device__ __forceinline__ void local_states(const Chunked& A, unsigned char (*lds)[(1 + PARTS) * kTile]) {
+__device__ __forceinline__ void local_states(const Chunked& A, unsigned char (*halves)[2][(1 + PARTS) * kTile]) {
   const int64_t bh = blockIdx.x / (A.P - 1);
-  const Segment<REV> G(A, bh, (int)(blockIdx.x - bh * (A.P - 1)));
-  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  Segment<REV> G(A, bh, (int)(blockIdx.x - bh * (A.P - 1)));
+  const int tid = threadIdx.x & 255, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int second = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 8);
+  unsigned char(*lds)[(1 + PARTS) * kTile] = halves[second];
+  const int half = max(G.c1 - G.c0 + 1, 0) / 2, middle = G.c0 + half;
+  // tokens of the second half; both walk `half` chunks, the second's last may be empty
+  const float behind = (float)max(min((int64_t)G.len, (int64_t)G.c1 * kC) - (int64_t)middle * kC, (int64_t)0);
+  if (second)
+    G.c0 = middle;
+  else
+    G.c1 = middle;
+  G.end = G.c0 + half;
   const Lanes L(tid & 63);
   const int ah = wave & 1, ch = wave >> 1, gr = tid & 7, r0 = tid >> 3;
   struct Rows {
@@ -449,15 +462,27 @@ __device__ __forceinline__ void local_states(const Chunked& A, unsigned char (*l
 #pragma unroll
         for (int x = 0; x < 16; ++x) S[x] += T[x];
       });
-  float* so = A.seg + (bh * A.P + G.p) * 4096 + (32 * ah + L.r) * 64 + 32 * ch + 16 * L.hf;
+  // (the tiles are free: the walks end on a barrier)
+  float* first = (float*)halves[0][0];
+  if (!second) {
 #pragma unroll
-  for (int x = 0; x < 16; x += 4) *(float4*)(so + x) = make_float4(S[x], S[x + 1], S[x + 2], S[x + 3]);
+    for (int x = 0; x < 16; ++x) first[x * 256 + tid] = S[x];
+  }
+  __syncthreads();
+  if (second) {
+    const float w = decay_pow(G.g, behind);
+    float* so = A.seg + (bh * A.P + G.p) * 4096 + (32 * ah + L.r) * 64 + 32 * ch + 16 * L.hf;
+#pragma unroll
+    for (int x = 0; x < 16; ++x) S[x] = fmaf(w, first[x * 256 + tid], S[x]);
+#pragma unroll
+    for (int x = 0; x < 16; x += 4) *(float4*)(so + x) = make_float4(S[x], S[x + 1], S[x + 2], S[x + 3]);
+  }
 }
 
 // grid (slices (P - 1), directions): a gradient needs the states of both walks.
 template <int PARTS>
-__global__ __launch_bounds__(256, PARTS == 2 ? 3 : 2) void k_lin_states(Chunked F, Chunked B) {
-  __shared__ __attribute__((aligned(16))) unsigned char lds[2][(1 + PARTS) * kTile];  // V, the decayed K's parts
+__global__ __launch_bounds__(512, 2) void k_lin_states(Chunked F, Chunked B) {
+  __shared__ __attribute__((aligned(16))) unsigned char lds[2][2][(1 + PARTS) * kTile];  // V, the decayed K's parts
   if (blockIdx.y == 0)
     local_states<false, PARTS>(F, lds);
   else
@@ -1116,19 +1141,31 @@ __global__ __launch_bounds__(256, 1) void k_lin_backward_f32(Walk32 Q, Walk32 K,
 struct Split {
   int P, cps;
 };
-// A slice is split only where the walks would not fill half of the compute
-// units: HBM serves the others' reads as fast, and the segments' states cost
-// another pass over two of the tensors (B H = 128, n = 8000: 121 us whole, 137
-// in two; B H = 32, n = 20000: 284 us whole, 87 in eight).  Four chunks at
-// least to a segment.
+// The number of segments with the least expected time, in us, among those whose
+// workgroups fit the GPU at once.  A walk is bound by the latency of its chunks
+// (0.8 us a chunk forward, 1.4 times that in the gradient's pair of walks) or by
+// HBM; segments take a launch and half a walk more for their states, and read
+// two of the tensors (four) again.  Measured, whole against split: B H = 128, n =
+// 8000: 120 and 137 us (two); B H = 32, n = 20000: 284 and 95 (eight); B H = 64, n
+// = 1024: 17.8 and 19.3 (four); B H = 2, n = 1024: 16.9 and 13.5 (eight).
 Split split_of(const LinearDims& d, int walks) {
   const int chunks = (d.n + kC - 1) / kC;
   const int64_t all = (int64_t)d.B * d.H * walks;
-  int64_t P = all >= 128 ? 1 : 256 / all;
-  if (P > chunks / 4) P = chunks / 4;
-  if (P < 1) P = 1;
-  const int cps = (int)((chunks + P - 1) / P);
-  return Split{(chunks + cps - 1) / cps, cps};
+  const double slow = walks == 1 ? 1.0 : 1.4, tensor = (double)d.B * d.H * d.n * 128 / 5.3e6;  // us of one tensor
+  Split best{1, chunks};
+  double least = 0;
+  for (int64_t P = 1; P == 1 || (P * all <= 256 && P <= chunks); ++P) {
+    const int cps = (int)((chunks + P - 1) / P);
+    if ((chunks + cps - 1) / cps != P) continue;
+    const double full = fmin((double)(P * all) / 256, 1);
+    const double walk = P == 1 ? 4.4 + cps * slow * (0.8 + 0.08 * full)
+                               : 7.6 + 3.7 * full + (P <= 8 ? 0.45 * P : 3.5 + 0.12 * P) +
+                                     cps * slow * (1.2 + 0.35 * full);
+    const double bytes = tensor * (walks == 1 ? (P == 1 ? 4 : 6) : (P == 1 ? 10 : 14));
+    const double us = fmax(walk, bytes) + 0.1 * walk;
+    if (P == 1 || us < least) best = Split{(int)P, cps}, least = us;
+  }
+  return best;
 }
 size_t seg_bytes(const LinearDims& d, Split s) {
   return s.P > 1 ? (size_t)d.B * d.H * s.P * 4096 * 4 : 0;
@@ -1150,9 +1187,9 @@ void segment_states(const LinearDims& d, const Chunked& f, const Chunked& b, uns
     TimedLaunch tl("lin_states", st);
     const dim3 grid(slices * (f.P - 1), directions);
     if (exact)
-      hipLaunchKernelGGL(k_lin_states<3>, grid, dim3(256), 0, st, f, b);
+      hipLaunchKernelGGL(k_lin_states<3>, grid, dim3(512), 0, st, f, b);
     else
-      hipLaunchKernelGGL(k_lin_states<2>, grid, dim3(256), 0, st, f, b);
+      hipLaunchKernelGGL(k_lin_states<2>, grid, dim3(512), 0, st, f, b);
   }
   if (f.scanned || b.scanned) {
     TimedLaunch tl("lin_scan", st);
@@ -1163,17 +1200,25 @@ void segment_states(const LinearDims& d, const Chunked& f, const Chunked& b, uns
   }
 }
 
-// fp32: a slice's two halves are a wave each, and one wave keeps a SIMD's
-// matrix unit busy (B H = 128, n = 4000: 195 us with one a SIMD, 206 with two,
-// 350 with half).  Two chunks of 64 at least to a segment.
+// fp32, in the same way: a slice's two halves are a wave each, and one wave keeps
+// a SIMD's matrix unit busy (B H = 128, n = 4000: 195 us with one a SIMD, 206 with
+// two, 350 with half), so 1024 waves are a round.  A chunk of 64 tokens takes a
+// walk 7.3 us and the states' pass 2.6.  Measured, whole against split: B H = 4,
+// n = 1024: 125 and 26 us (16 segments); gradient, B H = 96, n = 512: 70 and 78
+// (three), n = 4096: 507 and 448 (three).
 Split split32_of(const LinearDims& d, int walks) {
   const int chunks = (d.n + kC - 1) / kC;
-  const int64_t all = (int64_t)d.B * d.H * walks * 2;
-  int64_t P = all >= 768 ? 1 : 1024 / all;
-  if (P > chunks / 2) P = chunks / 2;
-  if (P < 1) P = 1;
-  const int cps = (int)((chunks + P - 1) / P);
-  return Split{(chunks + cps - 1) / cps, cps};
+  const int64_t waves = (int64_t)d.B * d.H * 2, states = walks == 1 ? 1 : 2;
+  Split best{1, chunks};
+  double least = 0;
+  for (int64_t P = 1; P == 1 || (P * waves * walks <= 2048 && P <= chunks); ++P) {
+    const int cps = (int)((chunks + P - 1) / P);
+    if ((chunks + cps - 1) / cps != P) continue;
+    const int64_t rounds = (P * waves * walks + 1023) / 1024, before = (P * waves * states + 1023) / 1024;
+    const double us = rounds * (4 + 7.3 * cps) + (P > 1 ? 5.2 + 0.15 * P + before * 2.6 * cps : 0);
+    if (P == 1 || us < least) best = Split{(int)P, cps}, least = us;
+  }
+  return best;
 }
 
 Walk32 walk32_of(const LinearDims& d, Split s, const float* log_decay, const int32_t* lengths, float scale) {
