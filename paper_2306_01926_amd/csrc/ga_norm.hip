@@ -543,34 +543,36 @@ __global__ __launch_bounds__(wg_threads(TPR)) void k_norm_grad(NormArgs<DT> A, c
   }
 }
 
-// out[g][col] = sum over parts p of src[(g parts + p) stride + col], in
-// ascending order within each of 64 interleaved shares.  grid (ceil(W / 16),
-// outputs, groups of the gate).
+// out[col] = sum over parts p of src[p stride + col] for the four parameters'
+// sums (of all workgroups) and each group's gate (of its workgroups): in
+// ascending order within each of the interleaved shares that a column's threads
+// take, 32 columns and up to 32 shares to a workgroup.  grid: ceil(W / 32)
+// blocks of columns, times 4 parameters and the groups.
 struct NormOuts {
   float* out[5];
 };
 __global__ __launch_bounds__(1024) void k_norm_params(const float* __restrict__ part, const float* __restrict__ gpart,
                                                       int wgs, int split, int W, NormOuts O) {
-  __shared__ float buf[64][17];
-  const int which = blockIdx.y;
-  float* out = O.out[which];
-  if (!out || (which != 4 && blockIdx.z > 0)) return;
-  const float* src = which == 4 ? gpart + (int64_t)blockIdx.z * split * W : part + (int64_t)which * W;
+  __shared__ float buf[32][33];
+  const int blocks = (W + 31) / 32, row = (int)(blockIdx.x / blocks), which = min(row, 4);
+  if (!O.out[which]) return;
+  const int64_t group = row - which;
+  float* out = O.out[which] + group * W;
+  const float* src = which == 4 ? gpart + group * split * W : part + (int64_t)which * W;
   const int64_t stride = which == 4 ? W : 4 * (int64_t)W;
-  const int count = which == 4 ? split : wgs;
-  const int cl = threadIdx.x & 15, s = threadIdx.x >> 4, col = blockIdx.x * 16 + cl;
+  const int count = which == 4 ? split : wgs, shares = blockDim.x >> 5;
+  const int cl = threadIdx.x & 31, s = threadIdx.x >> 5, col = (int)(blockIdx.x - (unsigned)row * blocks) * 32 + cl;
   float v = 0.f;
   if (col < W) {
 #pragma unroll 8
-    for (int p = s; p < count; p += 64) v += src[p * stride + col];
+    for (int p = s; p < count; p += shares) v += src[p * stride + col];
   }
   buf[s][cl] = v;
   __syncthreads();
   if (s == 0 && col < W) {
     float t = 0.f;
-#pragma unroll
-    for (int k = 0; k < 64; ++k) t += buf[k][cl];
-    out[(which == 4 ? (int64_t)blockIdx.z * W : 0) + col] = t;
+    for (int k = 0; k < shares; ++k) t += buf[k][cl];
+    out[col] = t;
   }
 }
 
@@ -681,8 +683,11 @@ hipError_t launch_norm_grad(const NormDims& d, const NormTensors& t, const void*
   if (params || gate) {
     TimedLaunch tl("norm_params", st);
     NormOuts o{{out[0], out[1], out[2], out[3], gate ? out[4] : nullptr}};
-    hipLaunchKernelGGL(k_norm_params, dim3((unsigned)((d.W + 15) / 16), 5, gate ? (unsigned)p.groups : 1u), dim3(1024),
-                       0, st, p.part, p.gpart, wgs, p.split, d.W, o);
+    // eight parts to a share, which are requested at once
+    unsigned shares = 2;
+    while (shares < 32 && shares * 8 < (unsigned)wgs) shares *= 2;
+    hipLaunchKernelGGL(k_norm_params, dim3((unsigned)((d.W + 31) / 32 * (gate ? 4 + p.groups : 4))), dim3(32 * shares), 0,
+                       st, p.part, p.gpart, wgs, p.split, d.W, o);
   }
   return hipGetLastError();
 }
