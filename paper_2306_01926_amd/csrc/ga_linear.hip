@@ -26,8 +26,6 @@ namespace {
 
 #include "ga_device.h"
 
-constexpr int kStep = 16;  // tokens staged at a time
-
 // The decay of a state value over some tokens, l^n x.  Many decays in a row
 // compound what the factor is off by, and 2^-24 of a factor near one is large
 // against its distance to one; l^n - 1 is formed without that loss, and l^n x
@@ -60,7 +58,8 @@ __device__ __forceinline__ int length_of(const int32_t* lengths, int64_t b, int 
 
 // One token per sequence: 256 threads per slice, thread (r, g) holds rows
 // r + 16 u of the state at columns 4 g .. 4 g + 3.  Bound by the state, 16 KB
-// read and 16 KB written per slice; everything is fp32.
+// read and 16 KB written per slice (B H = 2048: 11.4 us, 5.9 TB/s; B H = 2: 2.4
+// us); everything is fp32.
 template <class DT>
 __global__ __launch_bounds__(256) void k_lin_step(const typename DT::T* Q, const typename DT::T* K,
                                                   const typename DT::T* V, const float* log_decay,
@@ -169,8 +168,14 @@ __global__ __launch_bounds__(256) void k_lin_heads(const float* __restrict__ par
 // registers are the next product's operand as they are: no LDS round trip.
 // The value rows feeding the last product are permuted so that a lane ends with
 // 16 consecutive features of one token (32 bytes, stored from registers).
-// K and V rows sit in LDS as they come; the operands that need a column of them
-// come from transposing LDS reads.  Q goes to registers directly.
+// K, V and Q rows sit in LDS as they come; the operands that need a column of
+// them come from transposing LDS reads.
+//
+// B H = 128, n = 8000 (524 MB): 120 us, 4.4 TB/s, where a copy runs at 5.3; 160 us
+// with four waves for both jobs and rows one chunk ahead.  A walk takes 0.8 us a
+// chunk: the chain from one state to the next (conversion of the keys, an LDS
+// round trip, the products) beside four waves of output; so few slices are bound
+// by it, and are split, and many by HBM.
 //
 // Roundings: the scores after decay and the state that Q meets are rounded to
 // bf16, as the matrix cores need (each term of an output passes one of the
@@ -228,7 +233,7 @@ __device__ __forceinline__ void buf_store(Buffer b, int off, u32x4 x) {
 }
 
 struct Chunked {
-  const uint16_t *q, *k, *v, *w;                // roles (see the head of the file; w: k_lin_grad alone)
+  const uint16_t *q, *k, *v, *w;                // roles (see the head of the file; w: the gradient's backward walk alone)
   bool q_shared, k_shared, v_shared, w_shared;  // the tensor has Hk heads
   const float *log_decay, *state;
   const int32_t* lengths;
@@ -249,7 +254,7 @@ template <bool REV>
 struct Segment {
   const uint16_t *q, *k, *v, *w;
   int64_t bh;
-  int p, len, c0, c1, end;  // its chunks; where the walk ends
+  int p, len, c0, c1;
   float g, ld, ks;
 
   __device__ __forceinline__ Segment(const Chunked& A, int64_t slice, int segment) : bh(slice), p(segment) {
@@ -264,7 +269,7 @@ struct Segment {
     g = decay_log2(A.log_decay[h]);
     ks = REV ? A.scale : 1.f;
     c0 = p * A.cps;
-    c1 = end = min(c0 + A.cps, (len + kC - 1) / kC);
+    c1 = min(c0 + A.cps, (len + kC - 1) / kC);
   }
   // rows of chunk c (none behind the segment), the first one in memory, and
   // the place of walk row x among them (beyond them: out of the buffer)
@@ -307,7 +312,7 @@ struct Segment {
   // between them, which would cost copies of rows in flight (a wait for them).
   template <class Rows, class Load, class Put, class Step>
   __device__ __forceinline__ void walk(Load load, Put put, Step step) const {
-    if (c0 >= end) return;
+    if (c0 >= c1) return;
     Rows R0, R1, R2;
     load(c0, R0);
     load(c0 + 1, R1);
@@ -320,13 +325,13 @@ struct Segment {
       __syncthreads();
     };
     int c = c0, buf = 0;
-    for (; c + 3 <= end; c += 3, buf ^= 1) {
+    for (; c + 3 <= c1; c += 3, buf ^= 1) {
       turn(c, buf, R1, R0);
       turn(c + 1, buf ^ 1, R2, R1);
       turn(c + 2, buf, R0, R2);
     }
-    if (c < end) turn(c, buf, R1, R0);
-    if (c + 1 < end) turn(c + 1, buf ^ 1, R2, R1);
+    if (c < c1) turn(c, buf, R1, R0);
+    if (c + 1 < c1) turn(c + 1, buf ^ 1, R2, R1);
   }
 };
 
@@ -401,24 +406,12 @@ struct StateUpdate {
 };
 
 // The local states of the segments but the last, from zero: four waves, a
-// quadrant of the state each, walk the first half of a segment's chunks, four
-// more the second, and take the first half's state into theirs (one wave a SIMD
-// waits for its own LDS reads and products).
+// quadrant of the state each.
 template <bool REV, int PARTS>
-__device__ __forceinline__ void local_states(const Chunked& A, unsigned char (*halves)[2][(1 + PARTS) * kTile]) {
+__device__ __forceinline__ void local_states(const Chunked& A, unsigned char (*lds)[(1 + PARTS) * kTile]) {
   const int64_t bh = blockIdx.x / (A.P - 1);
-  Segment<REV> G(A, bh, (int)(blockIdx.x - bh * (A.P - 1)));
-  const int tid = threadIdx.x & 255, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int second = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 8);
-  unsigned char(*lds)[(1 + PARTS) * kTile] = halves[second];
-  const int half = max(G.c1 - G.c0 + 1, 0) / 2, middle = G.c0 + half;
-  // tokens of the second half; both walk `half` chunks, the second's last may be empty
-  const float behind = (float)max(min((int64_t)G.len, (int64_t)G.c1 * kC) - (int64_t)middle * kC, (int64_t)0);
-  if (second)
-    G.c0 = middle;
-  else
-    G.c1 = middle;
-  G.end = G.c0 + half;
+  const Segment<REV> G(A, bh, (int)(blockIdx.x - bh * (A.P - 1)));
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const Lanes L(tid & 63);
   const int ah = wave & 1, ch = wave >> 1, gr = tid & 7, r0 = tid >> 3;
   struct Rows {
@@ -462,27 +455,15 @@ __device__ __forceinline__ void local_states(const Chunked& A, unsigned char (*h
 #pragma unroll
         for (int x = 0; x < 16; ++x) S[x] += T[x];
       });
-  // (the tiles are free: the walks end on a barrier)
-  float* first = (float*)halves[0][0];
-  if (!second) {
+  float* so = A.seg + (bh * A.P + G.p) * 4096 + (32 * ah + L.r) * 64 + 32 * ch + 16 * L.hf;
 #pragma unroll
-    for (int x = 0; x < 16; ++x) first[x * 256 + tid] = S[x];
-  }
-  __syncthreads();
-  if (second) {
-    const float w = decay_pow(G.g, behind);
-    float* so = A.seg + (bh * A.P + G.p) * 4096 + (32 * ah + L.r) * 64 + 32 * ch + 16 * L.hf;
-#pragma unroll
-    for (int x = 0; x < 16; ++x) S[x] = fmaf(w, first[x * 256 + tid], S[x]);
-#pragma unroll
-    for (int x = 0; x < 16; x += 4) *(float4*)(so + x) = make_float4(S[x], S[x + 1], S[x + 2], S[x + 3]);
-  }
+  for (int x = 0; x < 16; x += 4) *(float4*)(so + x) = make_float4(S[x], S[x + 1], S[x + 2], S[x + 3]);
 }
 
 // grid (slices (P - 1), directions): a gradient needs the states of both walks.
 template <int PARTS>
-__global__ __launch_bounds__(512, 2) void k_lin_states(Chunked F, Chunked B) {
-  __shared__ __attribute__((aligned(16))) unsigned char lds[2][2][(1 + PARTS) * kTile];  // V, the decayed K's parts
+__global__ __launch_bounds__(256, PARTS == 2 ? 3 : 2) void k_lin_states(Chunked F, Chunked B) {
+  __shared__ __attribute__((aligned(16))) unsigned char lds[2][(1 + PARTS) * kTile];  // V, the decayed K's parts
   if (blockIdx.y == 0)
     local_states<false, PARTS>(F, lds);
   else
@@ -490,6 +471,8 @@ __global__ __launch_bounds__(512, 2) void k_lin_states(Chunked F, Chunked B) {
 }
 
 // Outputs of a forward walk (and the final state): workgroup `block` of slices P.
+// B H = 8, n = 100003: the states' pass over K and V 49 us (4.2 TB/s), the scan 7,
+// this 76 (5.4 TB/s).
 constexpr int forward_buf(int PARTS) { return (4 + PARTS) * kTile; }  // V, the state, Q, K, the decayed K's parts
 template <int PARTS>
 __device__ __forceinline__ void forward_walk(const Chunked& A, int block, unsigned char (*lds)[forward_buf(PARTS)]) {
@@ -706,7 +689,10 @@ __device__ __forceinline__ void forward_walk(const Chunked& A, int block, unsign
 // R[a][c] (a: feature of q and k, c: of v and dO), dK with its other side.
 // Eight waves: waves 0-3 form 32 tokens by 64 features of dV (0, 1) or dK
 // (2, 3), waves 4-7 the state.  out: dV, out2: dK; OUT32: they are fp32 (a
-// query head's share of a shared head's gradient).
+// query head's share of a shared head's gradient).  Both walks of the gradient
+// together are bound by HBM: they read seven tensors, the states' pass four, and
+// write three (B H = 32, n = 20000: 65 + 147 us, 5.4 TB/s; B H = 128, n = 8000, not
+// split: 257 us, 5.1 TB/s).
 constexpr int backward_buf(int PARTS) { return (5 + PARTS) * kTile; }  // dO, K, V, the state, Q, the decayed Q's parts
 template <bool OUT32, int PARTS>
 __device__ __forceinline__ void backward_walk(const Chunked& A, int block, unsigned char (*lds)[backward_buf(PARTS)]) {
@@ -952,7 +938,8 @@ __global__ __launch_bounds__(256) void k_lin_scan(Scan F, Scan B) {
 // the products are a quarter of the plain quadratic form's at 64 tokens, and
 // smaller chunks would add more to the state's products than they save.  Rows of
 // a later chunk are requested where the registers of this one's become free,
-// hundreds of cycles before their use.
+// hundreds of cycles before their use.  B H = 128, n = 4000: the outputs' walks
+// take 137 us, 93 of them at that rate.
 constexpr int kC32 = 32;
 
 struct Walk32 {
@@ -1187,9 +1174,9 @@ void segment_states(const LinearDims& d, const Chunked& f, const Chunked& b, uns
     TimedLaunch tl("lin_states", st);
     const dim3 grid(slices * (f.P - 1), directions);
     if (exact)
-      hipLaunchKernelGGL(k_lin_states<3>, grid, dim3(512), 0, st, f, b);
+      hipLaunchKernelGGL(k_lin_states<3>, grid, dim3(256), 0, st, f, b);
     else
-      hipLaunchKernelGGL(k_lin_states<2>, grid, dim3(512), 0, st, f, b);
+      hipLaunchKernelGGL(k_lin_states<2>, grid, dim3(256), 0, st, f, b);
   }
   if (f.scanned || b.scanned) {
     TimedLaunch tl("lin_scan", st);

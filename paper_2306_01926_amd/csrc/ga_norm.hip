@@ -17,7 +17,8 @@
 // reading a stored y), so nothing is kept from the forward pass.
 //
 // Both are bound by HBM: 4 rows of W values moved per token forward (x, f in,
-// y, h out), 6 backward.  A row lives in the registers of TPR threads, eight
+// y, h out), 6 backward (D = 512, 128000 tokens, bf16: 112 us, 4.7 TB/s; gradient
+// 166 us, 4.7 TB/s; a copy runs at 5.3).  A row lives in the registers of TPR threads, eight
 // consecutive features each, so it is read once; the variance is the mean
 // square about the mean, formed from those registers (two sums), all in fp32.
 // One wave holds a row of up to 512 features and reduces by lane exchanges
@@ -362,7 +363,7 @@ __device__ __forceinline__ void team_store(const float (&v)[kE], float* buf, flo
 // BIAS: the gradients of the norms' biases are asked for.
 // Threads of a team of 1024 have 128 registers each: they keep the sums in LDS,
 // read the parameters again (from the caches) where they use them and the rows
-// where they begin them (D = 8192, 4000 rows, bf16: 131 us, and 279 with all of
+// where they begin them (D = 8192, 4000 rows, bf16: 123 us, and 279 with all of
 // it in registers, most of them spilled).
 template <class DT, int TPR, bool VEC, bool BIAS>
 __global__ __launch_bounds__(wg_threads(TPR)) void k_norm_grad(NormArgs<DT> A, const typename DT::T* __restrict__ dY,
