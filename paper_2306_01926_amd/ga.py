@@ -179,6 +179,7 @@ def _check(rc: int):
 # lookup, and every call needs one or two: the smallest calls are bound by the
 # host); a torch without it takes the public way.
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)  # (the tensors are there already)
 
 
 def _stream_handle(device) -> int:
@@ -423,7 +424,7 @@ def backward(Q: torch.Tensor, dO: torch.Tensor, belong: torch.Tensor, centroid: 
 
 def _launch(dev, call, *args) -> None:
     """One entry point on the current stream of `dev`, with that device current."""
-    if dev.index is None or dev.index == torch.cuda.current_device():
+    if dev.index == _current_device() or dev.index is None:
         rc = call(*args, _stream_handle(dev))
     else:
         with torch.cuda.device(dev):
@@ -460,19 +461,24 @@ def _scratch(nbytes: int, dev, ws):
 
 @functools.lru_cache(maxsize=1024)
 def _linear_shape(B: int, H: int, Hk: int, n: int, d: int, dtype):
-    """(shape, forward workspace, backward workspace) of a call (the sizes depend on nothing else)."""
-    s = Shape(B, H, n, d, {torch.bfloat16: GA_BF16, torch.float32: GA_F32}[dtype])
-    return s, int(lib().ga_linear_workspace_bytes(s, Hk)), int(lib().ga_linear_backward_workspace_bytes(s, Hk))
+    """(shape, forward workspace, backward workspace, default scale) of a call, which depend on nothing else."""
+    if dtype not in (torch.bfloat16, torch.float32):
+        raise TypeError(f"unsupported dtype {dtype} (bf16 or fp32)")
+    s = Shape(B, H, n, d, GA_BF16 if dtype is torch.bfloat16 else GA_F32)
+    return (s, int(lib().ga_linear_workspace_bytes(s, Hk)), int(lib().ga_linear_backward_workspace_bytes(s, Hk)),
+            1.0 / math.sqrt(max(d, 1)))
 
 
 def _heads(Q, K, name: str):
     """(B, H, Hk, n, d, device, dtype) of queries [B,H,n,d] and keys [B,Hk,n,d]."""
-    dev = _qkv_like(Q, "Q")
-    if not isinstance(K, torch.Tensor) or K.dim() != 4:
-        raise ValueError(f"{name} must be a [B, Hk, n, d] tensor")
-    _dtype_code(Q)
-    B, H, n, d = Q.shape
-    return B, H, K.shape[1], n, d, dev, Q.dtype
+    if not isinstance(Q, torch.Tensor) or not isinstance(K, torch.Tensor) or len(qs := Q.shape) != 4 or \
+            len(ks := K.shape) != 4:
+        raise ValueError(f"Q must be a [B, H, n, d] and {name} a [B, Hk, n, d] tensor")
+    dev = Q.device
+    if dev.type != "cuda":
+        _device_of(Q)
+    B, H, n, d = qs
+    return B, H, ks[1], n, d, dev, Q.dtype
 
 
 def linear_workspace_bytes(shape: Shape, Hk: int) -> int:
@@ -495,10 +501,11 @@ def linear_attend(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, log_decay: 
     O = torch.empty_like(Q) if out is None else out
     if return_state and out_state is None:
         out_state = torch.empty(states, dtype=torch.float32, device=dev)
-    s, nbytes, _ = _linear_shape(B, H, Hk, n, d, dt)
+    s, nbytes, _, usual = _linear_shape(B, H, Hk, n, d, dt)
     ws, wp, nb = _scratch(nbytes, dev, ws)
-    _launch(dev, lib().ga_linear_attend, s, Hk, *pointers, 1.0 / math.sqrt(d) if scale is None else float(scale),
-            _at(O, "out", dev, dt, q), _maybe(out_state, "out_state", dev, torch.float32, states), wp, nb)
+    _launch(dev, lib().ga_linear_attend, s, Hk, *pointers, usual if scale is None else float(scale),
+            O.data_ptr() if out is None else _at(O, "out", dev, dt, q),
+            _maybe(out_state, "out_state", dev, torch.float32, states), wp, nb)
     return (O, out_state) if return_state else O
 
 
@@ -521,9 +528,9 @@ def linear_backward(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, dO: torch
                 _maybe(dstate, "dstate", dev, torch.float32, states))
     dQ, dK, dV = torch.empty_like(Q), torch.empty_like(K), torch.empty_like(V)
     out = torch.empty(states, dtype=torch.float32, device=dev) if return_dstate else None
-    s, _, nbytes = _linear_shape(B, H, Hk, n, d, dt)
+    s, _, nbytes, usual = _linear_shape(B, H, Hk, n, d, dt)
     ws, wp, nb = _scratch(nbytes, dev, ws)
-    _launch(dev, lib().ga_linear_backward, s, Hk, *pointers, 1.0 / math.sqrt(d) if scale is None else float(scale),
+    _launch(dev, lib().ga_linear_backward, s, Hk, *pointers, usual if scale is None else float(scale),
             dQ.data_ptr(), dK.data_ptr(), dV.data_ptr(), None if out is None else out.data_ptr(), wp, nb)
     return (dQ, dK, dV, out) if return_dstate else (dQ, dK, dV)
 
@@ -534,18 +541,20 @@ def linear_step(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, log_decay: to
     """One token per sequence (Q [B,H,1,64]) on kept states [states,H,64,64] fp32, updated in place unless out_state
     is given: (O, the updated states).  slots [B] int32: the state of each batch row (outside the states: padding)."""
     B, H, Hk, n, d, dev, dt = _heads(Q, K, "K")
-    if not isinstance(state, torch.Tensor) or state.dim() != 4:
+    if not isinstance(state, torch.Tensor) or len(state.shape) != 4:
         raise ValueError("state must be a [states, H, 64, 64] tensor")
     many = state.shape[0]
     q, kv, states = (B, H, n, d), (B, Hk, n, d), (many, H, d, d)
+    s, _, _, usual = _linear_shape(B, H, Hk, n, d, dt)
     O = torch.empty_like(Q) if out is None else out
+    at = _at(state, "state", dev, torch.float32, states)
     if out_state is None:
         out_state = state
-    _launch(dev, lib().ga_linear_step, _linear_shape(B, H, Hk, n, d, dt)[0], Hk, _at(Q, "Q", dev, dt, q),
-            _at(K, "K", dev, dt, kv), _at(V, "V", dev, dt, kv), _at(log_decay, "log_decay", dev, torch.float32, (H,)),
-            _maybe(slots, "slots", dev, torch.int32, (B,)), many, _at(state, "state", dev, torch.float32, states),
-            1.0 / math.sqrt(d) if scale is None else float(scale), _at(O, "out", dev, dt, q),
-            _at(out_state, "out_state", dev, torch.float32, states))
+    _launch(dev, lib().ga_linear_step, s, Hk, _at(Q, "Q", dev, dt, q), _at(K, "K", dev, dt, kv),
+            _at(V, "V", dev, dt, kv), _at(log_decay, "log_decay", dev, torch.float32, (H,)),
+            _maybe(slots, "slots", dev, torch.int32, (B,)), many, at, usual if scale is None else float(scale),
+            O.data_ptr() if out is None else _at(O, "out", dev, dt, q),
+            at if out_state is state else _at(out_state, "out_state", dev, torch.float32, states))
     return O, out_state
 
 
@@ -584,6 +593,9 @@ def rotary(Q: torch.Tensor, K: torch.Tensor | None, pos: torch.Tensor, pairs, ba
 NORMS = {"rms": 0, "layer": 1}
 
 
+_norm_shape = functools.lru_cache(maxsize=1024)(Norm)  # (0.7 us less than a new one)
+
+
 def _norm_args(X, F, norm, eps, post_weight, post_bias, gate, pre_weight, pre_bias, residual_scale, branch_scale):
     """Checks shared by the norm's calls; (ga_norm_t, device, dtype, the tensors' addresses)."""
     if not isinstance(X, torch.Tensor) or X.dim() != 3:
@@ -598,7 +610,8 @@ def _norm_args(X, F, norm, eps, post_weight, post_bias, gate, pre_weight, pre_bi
             raise ValueError("gate must be a [D] or [B, D] tensor")
         batches = 1 if gate.dim() == 1 else B
         g = _at(gate, "gate", dev, dt, (D,) if gate.dim() == 1 else (B, D))
-    s = Norm(B, n, D, code, NORMS[norm], batches, eps, residual_scale, branch_scale)
+    # (+ 0.0: of two equal zeros one is kept)
+    s = _norm_shape(B, n, D, code, NORMS[norm], batches, eps, residual_scale + 0.0, branch_scale + 0.0)
     w = (D,)
     return s, dev, dt, (_at(X, "X", dev, dt, (B, n, D)), _maybe(F, "F", dev, dt, (B, n, D)),
                         _maybe(post_weight, "post_weight", dev, dt, w), _maybe(post_bias, "post_bias", dev, dt, w), g,
