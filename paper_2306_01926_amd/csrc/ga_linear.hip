@@ -924,22 +924,24 @@ __global__ __launch_bounds__(256) void k_lin_scan(Scan F, Scan B) {
 
 // ---------------------------------------------------------------- fp32, by chunks
 //
-// The same by chunks of 32 tokens with the fp32 matrix instructions (32x32x2):
-// one operand value per lane and step, so the registers that hold a result are
-// an operand of the next product in any of the roles that the walk needs.  With
-// (r, hf) the lane and j(x) = 8 (x / 4) + 4 hf + x % 4 for x = 0..15:
+// The same by chunks of 32 tokens, every operand as three bf16 parts and every
+// product as six (24 bits; the fp32 matrix instructions take 64 cycles for two
+// features where the six take 192 for sixteen).  A register that holds a result
+// is an operand of the next product in any of the roles that the walk needs.
+// With (r, hf) the lane and j(x) = 8 (x / 4) + 4 hf + x % 4 for x = 0..15:
 //   lane r holds K[r][j(x)], Q[r][j(x)] (features j(x) and 32 + j(x)),
-//   V[j(x)][r], K[j(x)][r] (tokens j(x)), S[j(x)][r] (features of k),
-//   scores^T[j(x)][r], O^T[j(x)][r].
-// Only the decayed keys, needed by column, pass through LDS.  A wave walks a
-// segment for one half of the value features without a barrier; a workgroup is
-// the halves of two segments, so that its waves take a SIMD each.
-// Bound by the matrix instructions' rate, 112 of 64 cycles per chunk and half:
-// the products are a quarter of the plain quadratic form's at 64 tokens, and
-// smaller chunks would add more to the state's products than they save.  Rows of
-// a later chunk are requested where the registers of this one's become free,
-// hundreds of cycles before their use.  B H = 128, n = 4000: the outputs' walks
-// take 137 us, 93 of them at that rate.
+//   V[j(x)][r] (tokens j(x)), S[j(x)][r] (features of k), scores^T[j(x)][r],
+//   O^T[j(x)][r],
+// eight of which in order are the contracted values of one product.  Only the
+// keys, needed by column for the state, pass through LDS; the decay to the
+// chunk's end is on the values there.  A wave walks a segment for one half of
+// the value features without a barrier; a workgroup is the halves of two
+// segments.
+// A chunk takes 3.2 us: 84 matrix instructions of 32 cycles and 900 of the VALU
+// that make the parts, one after the other for the most part (3.6 us with the
+// fp32 instructions, 112 of 64 cycles).  B H = 24, n = 1111, gradient: 47 us, 51
+// with those.  Rows of a later chunk are requested where the registers of this
+// one's become free, hundreds of cycles before their use.
 constexpr int kC32 = 32;
 
 struct Walk32 {
@@ -953,19 +955,46 @@ struct Walk32 {
   bool transposed;  // the state and seg are S^T in this walk's roles
 };
 
-__device__ __forceinline__ f32x16 mfma1(float a, float b, const f32x16& c) {
-  return __builtin_amdgcn_mfma_f32_32x32x2f32(a, b, c, 0, 0, 0);
+// Eight fp32 values as three bf16 parts each (24 significant bits; exact but for
+// values below 2^-110, whose last bits lie below the type's range, and above
+// 3.38e38, which round to infinity), and the six products of parts that 24 bits
+// of a product need (what is left out is 2^-24 of it).
+struct Split8 {
+  u32x4 p[3];
+};
+template <class F>
+__device__ __forceinline__ Split8 split8(F value) {
+  Split8 s;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    float a = value(2 * e), b = value(2 * e + 1);
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+      s.p[i][e] = pack_bf16x2(a, b);
+      a -= __uint_as_float(s.p[i][e] << 16);
+      b -= __uint_as_float(s.p[i][e] & 0xffff0000u);
+    }
+  }
+  return s;
+}
+__device__ __forceinline__ f32x16 mfma6(const Split8& a, const Split8& b, f32x16 c) {
+  c = mfma(a.p[2], b.p[0], c);
+  c = mfma(a.p[0], b.p[2], c);
+  c = mfma(a.p[1], b.p[1], c);
+  c = mfma(a.p[1], b.p[0], c);
+  c = mfma(a.p[0], b.p[1], c);
+  return mfma(a.p[0], b.p[0], c);
 }
 __device__ __forceinline__ float buf_load1(Buffer b, int off) {
   return __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(b, off, 0, 0));
 }
 
-constexpr int kRow32 = 68;  // LDS row stride (floats): 16 rows' writes of 16 bytes meet all banks
-constexpr int kLds32 = kC32 * kRow32;
+constexpr int kPart32 = kC32 * 128;  // bytes of a chunk's keys, one part
+constexpr int kLds32 = 3 * kPart32;  // of a wave
 
 // Segments 2 block and 2 block + 1 of `items` in all (STATES: without each slice's last).
 template <bool REV, bool STATES>
-__device__ __forceinline__ void walk32(const Walk32& A, int block, int items, float (*lds)[kLds32]) {
+__device__ __forceinline__ void walk32(const Walk32& A, int block, int items, unsigned char (*lds)[kLds32]) {
   const int nseg = STATES ? A.P - 1 : A.P;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), item = 2 * block + (wave >> 1);
   if (item >= items) return;  // (no barriers)
@@ -975,7 +1004,8 @@ __device__ __forceinline__ void walk32(const Walk32& A, int block, int items, fl
   const int len = __builtin_amdgcn_readfirstlane(length_of(A.lengths, b, A.n));
   const int lane = threadIdx.x & 63, r = lane & 31, hf = lane >> 5;
   const int ch = wave & 1;
-  float* kt = lds[wave];  // the decayed keys, a token a row
+  unsigned char* kt = lds[wave];  // the keys' parts, a token a row
+  const Lanes L(lane);
   const float* q = A.q + (A.q_shared ? bk : bh) * A.n * 64;
   const float* k = A.k + (A.k_shared ? bk : bh) * A.n * 64;
   const float* v = A.v + (A.v_shared ? bk : bh) * A.n * 64 + 32 * ch;
@@ -1013,14 +1043,6 @@ __device__ __forceinline__ void walk32(const Walk32& A, int block, int items, fl
 #pragma unroll
     for (int x = 0; x < 16; ++x) vc[x] = buf_load1(bv, place(jx(x), nr) * 256 + 4 * r);
   };
-  auto put_keys = [&](int nr) __attribute__((always_inline)) {
-    const float w = ks * decay_pow(g, (float)(max(nr - 1 - r, 0) + REV));  // (rows behind the end are zeros)
-#pragma unroll
-    for (int u = 0; u < 8; ++u)
-      *(float4*)(kt + r * kRow32 + 8 * u + 4 * hf) =
-          make_float4(w * ka[4 * u], w * ka[4 * u + 1], w * ka[4 * u + 2], w * ka[4 * u + 3]);
-  };
-
   f32x16 S[2] = {zero16(), zero16()};  // S[32 e + j(x)][32 ch + r]
   if (!STATES) {
     const float* s0 = A.P > 1 ? A.seg + (bh * A.P + p) * 4096 : (A.state ? A.state + bh * 4096 : nullptr);
@@ -1041,6 +1063,14 @@ __device__ __forceinline__ void walk32(const Walk32& A, int block, int items, fl
   for (int x = 0; x < 16; ++x) wd[x] = r >= jx(x) ? A.scale * decay_pow(g, (float)(r - jx(x))) : 0.f;
   const float wi = (REV ? 1.f : A.scale) * decay_pow(g, (float)(r + 1 - REV));
 
+  // decay of each value row to the chunk's end
+  float wv[16];
+  auto to_end = [&](int nr) __attribute__((always_inline)) {
+#pragma unroll
+    for (int x = 0; x < 16; ++x) wv[x] = ks * decay_pow(g, (float)(max(nr - 1 - jx(x), 0) + REV));
+  };
+  to_end(kC32);
+
   if (t0 < t1) {
     load_row(k, t0, ka);
     if (!STATES) load_row(q, t0, qa);
@@ -1048,21 +1078,35 @@ __device__ __forceinline__ void walk32(const Walk32& A, int block, int items, fl
   }
   for (int64_t t = t0; t < t1; t += kC32) {
     const int nr = count(t);
-    f32x16 P = zero16(), oi = zero16(), o = zero16();
-    if (!STATES) {
+    if (nr < kC32) to_end(nr);  // (the last chunk; rows behind the end are zeros)
+    f32x16 P = zero16();
+    Split8 qp[4];
 #pragma unroll
-      for (int x = 0; x < 32; ++x) P = mfma1(ka[x], qa[x], P);
+    for (int s = 0; s < 4; ++s) {
+      const Split8 kp = split8([&](int e) { return ka[8 * s + e]; });
+#pragma unroll
+      for (int i = 0; i < 3; ++i) {
+        *(u32x2*)(kt + i * kPart32 + toff(r, 2 * s) + 8 * hf) = u32x2{kp.p[i][0], kp.p[i][1]};
+        *(u32x2*)(kt + i * kPart32 + toff(r, 2 * s + 1) + 8 * hf) = u32x2{kp.p[i][2], kp.p[i][3]};
+      }
+      if (!STATES) {
+        qp[s] = split8([&](int e) { return qa[8 * s + e]; });
+        P = mfma6(kp, qp[s], P);
+      }
     }
-    put_keys(nr);
     load_row(k, t + kC32, ka);
     __builtin_amdgcn_sched_barrier(0);  // (or the compiler requests everything at the end)
     if (!STATES) {
+      f32x16 oi = zero16(), o = zero16();
 #pragma unroll
-      for (int x = 0; x < 32; ++x) oi = mfma1(S[x / 16][x % 16], qa[x], oi);
+      for (int s = 0; s < 4; ++s)
+        oi = mfma6(split8([&](int e) { return S[s / 2][8 * (s % 2) + e]; }), qp[s], oi);
       load_row(q, t + kC32, qa);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int x = 0; x < 16; ++x) o = mfma1(vc[x], P[x] * wd[x], o);
+      for (int u = 0; u < 2; ++u)
+        o = mfma6(split8([&](int e) { return vc[8 * u + e]; }),
+                  split8([&](int e) { return P[8 * u + e] * wd[8 * u + e]; }), o);
       const Buffer bo = rows(out, t, nr);
       const int row = place(r, nr) * 256 + 16 * hf;
 #pragma unroll
@@ -1072,7 +1116,6 @@ __device__ __forceinline__ void walk32(const Walk32& A, int block, int items, fl
         for (int e = 0; e < 4; ++e) y[e] = __float_as_uint(fmaf(wi, oi[x + e], o[x + e]));
         buf_store(bo, row + 8 * x, y);
       }
-      __builtin_amdgcn_sched_barrier(0);
     }
     const float w = nr < kC32 ? decay_pow(g, (float)nr) : whole.next();
 #pragma unroll
@@ -1080,9 +1123,17 @@ __device__ __forceinline__ void walk32(const Walk32& A, int block, int items, fl
 #pragma unroll
       for (int x = 0; x < 16; ++x) S[e][x] *= w;
 #pragma unroll
-    for (int x = 0; x < 16; ++x)
+    for (int u = 0; u < 2; ++u) {
+      const Split8 vd = split8([&](int e) { return vc[8 * u + e] * wv[8 * u + e]; });
 #pragma unroll
-      for (int e = 0; e < 2; ++e) S[e] = mfma1(kt[jx(x) * kRow32 + 32 * e + r], vc[x], S[e]);
+      for (int e = 0; e < 2; ++e) {
+        Split8 kf;
+#pragma unroll
+        for (int i = 0; i < 3; ++i)
+          kf.p[i] = join(L.nat(kt + i * kPart32, 16 * u + 4 * hf, e), L.nat(kt + i * kPart32, 16 * u + 8 + 4 * hf, e));
+        S[e] = mfma6(kf, vd, S[e]);
+      }
+    }
     load_values(t + kC32);
     __builtin_amdgcn_sched_barrier(0);
   }
@@ -1103,20 +1154,20 @@ __device__ __forceinline__ void walk32(const Walk32& A, int block, int items, fl
 
 // grid (segments but each slice's last / 2, directions): the local states of forward and backward walks.
 __global__ __launch_bounds__(256, 1) void k_lin_states_f32(Walk32 F, Walk32 B, int items) {
-  __shared__ __attribute__((aligned(16))) float lds[4][kLds32];
+  __shared__ __attribute__((aligned(16))) unsigned char lds[4][kLds32];
   if (blockIdx.y == 0)
     walk32<false, true>(F, blockIdx.x, items, lds);
   else
     walk32<true, true>(B, blockIdx.x, items, lds);
 }
 // grid segments / 2.
-__global__ __launch_bounds__(256, 1) void k_lin_forward_f32(Walk32 A, int items) {
-  __shared__ __attribute__((aligned(16))) float lds[4][kLds32];
+__global__ __launch_bounds__(256, 2) void k_lin_forward_f32(Walk32 A, int items) {
+  __shared__ __attribute__((aligned(16))) unsigned char lds[4][kLds32];
   walk32<false, false>(A, blockIdx.x, items, lds);
 }
 // grid (segments / 2, walks): dQ, dK, dV from walk `from` on.
-__global__ __launch_bounds__(256, 1) void k_lin_backward_f32(Walk32 Q, Walk32 K, Walk32 V, int from, int items) {
-  __shared__ __attribute__((aligned(16))) float lds[4][kLds32];
+__global__ __launch_bounds__(256, 2) void k_lin_backward_f32(Walk32 Q, Walk32 K, Walk32 V, int from, int items) {
+  __shared__ __attribute__((aligned(16))) unsigned char lds[4][kLds32];
   const int walk = from + blockIdx.y;
   if (walk == 0)
     walk32<false, false>(Q, blockIdx.x, items, lds);
@@ -1187,23 +1238,26 @@ void segment_states(const LinearDims& d, const Chunked& f, const Chunked& b, uns
   }
 }
 
-// fp32, in the same way: a slice's two halves are a wave each, and one wave keeps
-// a SIMD's matrix unit busy (B H = 128, n = 4000: 195 us with one a SIMD, 206 with
-// two, 350 with half), so 1024 waves are a round.  A chunk of 64 tokens takes a
-// walk 7.3 us and the states' pass 2.6.  Measured, whole against split: B H = 4,
-// n = 1024: 125 and 26 us (16 segments); gradient, B H = 96, n = 512: 70 and 78
-// (three), n = 4096: 507 and 448 (three).
+// fp32, in the same way: a slice's two halves are a wave each, and 1024 waves, one
+// a SIMD, are a round (two waves a SIMD take nearly twice as long as one).  A
+// chunk of 64 tokens takes a walk 6.1 us and the states' pass 2.0, more where all
+// SIMDs work.  Measured, whole against split: B H = 16, n = 1024: 102 and 25 us (16
+// segments); gradient, B H = 64, n = 256: 33 and 36 (two), n = 4096: 425 and 268
+// (eight); B H = 128, n = 1024: 117 and 134 (four).
 Split split32_of(const LinearDims& d, int walks) {
   const int chunks = (d.n + kC - 1) / kC;
-  const int64_t waves = (int64_t)d.B * d.H * 2, states = walks == 1 ? 1 : 2;
+  const double waves = 2.0 * d.B * d.H / 1024;
+  const auto rounds = [](double w) { return w <= 1 ? 1 : 0.5 * (w + ceil(w)); };
   Split best{1, chunks};
   double least = 0;
-  for (int64_t P = 1; P == 1 || (P * waves * walks <= 2048 && P <= chunks); ++P) {
-    const int cps = (int)((chunks + P - 1) / P);
+  for (int P = 1; P == 1 || (P * waves * walks <= 6 && P <= chunks); ++P) {
+    const int cps = (chunks + P - 1) / P;
     if ((chunks + cps - 1) / cps != P) continue;
-    const int64_t rounds = (P * waves * walks + 1023) / 1024, before = (P * waves * states + 1023) / 1024;
-    const double us = rounds * (4 + 7.3 * cps) + (P > 1 ? 5.2 + 0.15 * P + before * 2.6 * cps : 0);
-    if (P == 1 || us < least) best = Split{(int)P, cps}, least = us;
+    const double main = P * waves * walks, before = P * waves * (walks == 1 ? 1 : 2);
+    const double us = P == 1 ? 4 + cps * rounds(main) * (6.1 + 0.7 * fmin(main, 1))
+                             : 11.4 + 0.13 * P + cps * (rounds(main) * (6.1 + 0.7 * fmin(main, 1)) +
+                                                        rounds(before) * (2.0 + 3.2 * fmin(before, 1)));
+    if (P == 1 || us < least) best = Split{P, cps}, least = us;
   }
   return best;
 }
