@@ -1192,9 +1192,8 @@ Split split_of(const LinearDims& d, int walks) {
   const double slow = walks == 1 ? 1.0 : 1.4, tensor = (double)d.B * d.H * d.n * 128 / 5.3e6;  // us of one tensor
   Split best{1, chunks};
   double least = 0;
-  for (int64_t P = 1; P == 1 || (P * all <= 256 && P <= chunks); ++P) {
+  for (int64_t P = 1; P == 1 || P * all <= 256;) {
     const int cps = (int)((chunks + P - 1) / P);
-    if ((chunks + cps - 1) / cps != P) continue;
     const double full = fmin((double)(P * all) / 256, 1);
     const double walk = P == 1 ? 4.4 + cps * slow * (0.8 + 0.08 * full)
                                : 7.6 + 3.7 * full + (P <= 8 ? 0.45 * P : 3.5 + 0.12 * P) +
@@ -1202,6 +1201,8 @@ Split split_of(const LinearDims& d, int walks) {
     const double bytes = tensor * (walks == 1 ? (P == 1 ? 4 : 6) : (P == 1 ? 10 : 14));
     const double us = fmax(walk, bytes) + 0.1 * walk;
     if (P == 1 || us < least) best = Split{(int)P, cps}, least = us;
+    if (cps == 1) break;
+    P = (chunks + cps - 2) / (cps - 1);  // the fewest segments of fewer chunks
   }
   return best;
 }
@@ -1250,14 +1251,15 @@ Split split32_of(const LinearDims& d, int walks) {
   const auto rounds = [](double w) { return w <= 1 ? 1 : 0.5 * (w + ceil(w)); };
   Split best{1, chunks};
   double least = 0;
-  for (int P = 1; P == 1 || (P * waves * walks <= 6 && P <= chunks); ++P) {
+  for (int P = 1; P == 1 || P * waves * walks <= 6;) {
     const int cps = (chunks + P - 1) / P;
-    if ((chunks + cps - 1) / cps != P) continue;
     const double main = P * waves * walks, before = P * waves * (walks == 1 ? 1 : 2);
     const double us = P == 1 ? 4 + cps * rounds(main) * (6.1 + 0.7 * fmin(main, 1))
                              : 11.4 + 0.13 * P + cps * (rounds(main) * (6.1 + 0.7 * fmin(main, 1)) +
                                                         rounds(before) * (2.0 + 3.2 * fmin(before, 1)));
     if (P == 1 || us < least) best = Split{P, cps}, least = us;
+    if (cps == 1) break;
+    P = (chunks + cps - 2) / (cps - 1);
   }
   return best;
 }

@@ -48,22 +48,24 @@ struct Tile {
     else
       return __uint_as_float(w[e]);
   }
-  // halves: si is negated in the first half's threads
-  __device__ __forceinline__ void turn(const float (&co)[kPairs], const float (&si)[kPairs], typename DT::T* p) const {
+  // halves: si is negated in the first half's threads; same: the pair stays as it
+  // is, whatever it holds (zero times infinity is not zero)
+  __device__ __forceinline__ void turn(const float (&co)[kPairs], const float (&si)[kPairs],
+                                       const bool (&same)[kPairs], typename DT::T* p) const {
     float v[kPer];
     if constexpr (INTERLEAVED) {
 #pragma unroll
       for (int m = 0; m < kPairs; ++m) {
         const float a = value(w, 2 * m), c = value(w, 2 * m + 1);
-        v[2 * m] = a * co[m] - c * si[m];
-        v[2 * m + 1] = c * co[m] + a * si[m];
+        v[2 * m] = same[m] ? a : a * co[m] - c * si[m];
+        v[2 * m + 1] = same[m] ? c : c * co[m] + a * si[m];
       }
     } else {
       u32x4 o;
 #pragma unroll
       for (int e = 0; e < 4; ++e) o[e] = (uint32_t)dpp<kThreads == 8 ? kHalfMirror : kMirror>((int)w[e]);
 #pragma unroll
-      for (int m = 0; m < kPairs; ++m) v[m] = value(w, m) * co[m] + value(o, m) * si[m];
+      for (int m = 0; m < kPairs; ++m) v[m] = same[m] ? value(w, m) : value(w, m) * co[m] + value(o, m) * si[m];
     }
     u32x4 o;
 #pragma unroll
@@ -100,6 +102,7 @@ __global__ __launch_bounds__(256) void k_rotary(const typename DT::T* Q, const t
   request(blockIdx.y, x[0]);
   request(blockIdx.y + step, x[1]);
   float co[R::kPairs], si[R::kPairs];
+  bool same[R::kPairs];
 #pragma unroll
   for (int e = 0; e < R::kPairs; ++e) {
     const int i = R::pair0(s) + e;
@@ -110,6 +113,7 @@ __global__ __launch_bounds__(256) void k_rotary(const typename DT::T* Q, const t
     si[e] = __builtin_amdgcn_sinf(f);  // of f turns; off by at most 2^-23 there (measured over 2^22 values)
     co[e] = __builtin_amdgcn_cosf(f);
     if (!INTERLEAVED && !R::second(s)) si[e] = -si[e];
+    same[e] = P.turns[i] == 0.0;
   }
   for (int h = blockIdx.y; h < heads; h += 2 * step) {
 #pragma unroll
@@ -118,7 +122,7 @@ __global__ __launch_bounds__(256) void k_rotary(const typename DT::T* Q, const t
       if (g >= heads) break;
       const R now = x[u];
       request(g + 2 * step, x[u]);
-      now.turn(co, si, (g < H ? Qo : Ko) + row(g));
+      now.turn(co, si, same, (g < H ? Qo : Ko) + row(g));
     }
   }
 }

@@ -197,7 +197,7 @@ def test_long_memory(dev, dtype, B, H, n, ends):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("B,H,n", [(1, 1, 5000), (2, 2, 333), (32, 8, 70)])
+@pytest.mark.parametrize("B,H,n", [(1, 1, 5000), (4, 8, 2000), (2, 2, 333), (32, 8, 70)])
 def test_states_in_place(dev, dtype, B, H, n):
     """A state given and handed back in one buffer, split over many segments, a few and none: the same values."""
     say(f"linear {dtype} states in place B={B} H={H} n={n}")

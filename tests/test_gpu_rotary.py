@@ -4,6 +4,8 @@ Error bar: the sine and cosine of an angle reduced in fp64 carry an absolute
 error below 2^-22, and the turn two fp32 products and a sum: 2^-21 (|a| + |b|)
 for a pair (a, b); a bf16 result is rounded once more, by 2^-8 of its value.
 """
+import math
+
 import pytest
 import torch
 
@@ -96,3 +98,21 @@ def test_many_heads_and_tokens(dev):
         whole, _ = ga.rotary(Q, Q, pos, (32,))
         part = ga.rotary(Q[:, 1:2, -50:].contiguous(), None, pos[:, :, -50:].contiguous(), (32,))
         assert torch.equal(whole[:, 1:2, -50:], part)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_copied_pairs_bit_for_bit(dev, dtype, interleaved):
+    """Pairs behind the last axis' are copied, infinities, NaN and the sign of zeros included."""
+    g = torch.Generator().manual_seed(3)
+    Q = torch.randn(2, 3, 40, 64, generator=g)
+    last = list(range(60, 64)) if interleaved else [30, 31, 62, 63]
+    for i, x in enumerate((math.inf, -0.0, -math.inf, math.nan)):
+        Q[:, :, ::2, last[i]] = x
+    Q = Q.to(DT[dtype]).to(dev)
+    pos = torch.arange(40, dtype=torch.int32, device=dev).view(1, 1, 40)
+    got = ga.rotary(Q, None, pos, (30,), interleaved=interleaved)
+    bits = torch.int16 if dtype == "bf16" else torch.int32
+    assert torch.equal(got[..., last].contiguous().view(bits), Q[..., last].contiguous().view(bits))
+    rest = [i for i in range(64) if i not in last]
+    assert torch.isfinite(got[..., rest]).all()
