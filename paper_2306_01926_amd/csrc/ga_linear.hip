@@ -233,7 +233,7 @@ __device__ __forceinline__ void buf_store(Buffer b, int off, u32x4 x) {
 }
 
 struct Chunked {
-  const uint16_t *q, *k, *v, *w;                // roles (see the head of the file; w: the gradient's backward walk alone)
+  const uint16_t *q, *k, *v, *w;                // roles (see the head of the file; w: the gradient's backward walk)
   bool q_shared, k_shared, v_shared, w_shared;  // the tensor has Hk heads
   const float *log_decay, *state;
   const int32_t* lengths;

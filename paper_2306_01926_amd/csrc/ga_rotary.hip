@@ -24,7 +24,8 @@ namespace {
 #include "ga_device.h"
 
 // A thread takes 16 bytes of a row, so that a wave's loads are whole rows
-// (107 us at B H = 128, n = 8000 against 110 with two loads of half rows).
+// (107 us at B H = 128, n = 8000 against 110 with two loads of half rows, both
+// through the caches).
 // Interleaved, its values are pairs; in the halves' layout they are one side of
 // as many pairs, whose other side the mirrored thread of the row holds: thread s
 // of T has values kPer s of the first half, thread T - 1 - s those of the second.
@@ -50,6 +51,7 @@ struct Tile {
   }
   // halves: si is negated in the first half's threads; same: the pair stays as it
   // is, whatever it holds (zero times infinity is not zero)
+  template <bool PAST>
   __device__ __forceinline__ void turn(const float (&co)[kPairs], const float (&si)[kPairs],
                                        const bool (&same)[kPairs], typename DT::T* p) const {
     float v[kPer];
@@ -75,13 +77,17 @@ struct Tile {
       else
         o[e] = __float_as_uint(v[e]);
     }
-    *(u32x4*)p = o;
+    if constexpr (PAST)
+      __builtin_nontemporal_store(o, (u32x4*)p);
+    else
+      *(u32x4*)p = o;
   }
 };
 
 // grid (ceil(n / kTokens), head shares, B).  Workgroup y takes heads y, y + gridDim.y, ...
-// of the H query heads followed by the Hk key heads.
-template <class DT, bool INTERLEAVED>
+// of the H query heads followed by the Hk key heads.  PAST: the outputs are
+// written past the caches.
+template <class DT, bool INTERLEAVED, bool PAST>
 __global__ __launch_bounds__(256) void k_rotary(const typename DT::T* Q, const typename DT::T* K, const void* pos,
                                                 RotaryPlan P, int H, int Hk, int n, typename DT::T* Qo,
                                                 typename DT::T* Ko) {
@@ -122,7 +128,7 @@ __global__ __launch_bounds__(256) void k_rotary(const typename DT::T* Q, const t
       if (g >= heads) break;
       const R now = x[u];
       request(g + 2 * step, x[u]);
-      now.turn(co, si, same, (g < H ? Qo : Ko) + row(g));
+      now.template turn<PAST>(co, si, same, (g < H ? Qo : Ko) + row(g));
     }
   }
 }
@@ -141,17 +147,29 @@ hipError_t launch_rotary(int dtype, int B, int H, int Hk, int n, const void* Q, 
   int64_t shares = (1024 + wgs - 1) / wgs;
   if (shares > heads) shares = heads;
   const dim3 grid(tiles, (unsigned)shares, (unsigned)B);
+  // Outputs that the last-level cache (256 MiB) holds are left to it, for whoever
+  // reads them next; more than three quarters of it would only drive each other
+  // out.  With the attention that reads them, bf16, B H = 128, n = 8000 (262 MB):
+  // 227 us past the caches and 231 through them, alone 103 and 107; B H = 64 (131
+  // MB): 125 and 123.
+  const bool past = (int64_t)B * heads * n * (dtype == 1 ? 128 : 256) > (192 << 20);
   TimedLaunch tl("rotary", st);
-#define GA_ROT(DT, I)                                                                                            \
-  hipLaunchKernelGGL((k_rotary<DT, I>), grid, dim3(256), 0, st, (const typename DT::T*)Q,                          \
+#define GA_ROT(DT, I, PAST)                                                                                      \
+  hipLaunchKernelGGL((k_rotary<DT, I, PAST>), grid, dim3(256), 0, st, (const typename DT::T*)Q,                    \
                      (const typename DT::T*)K, pos, plan, H, Hk, n, (typename DT::T*)Qo, (typename DT::T*)Ko)
+#define GA_ROT_PAST(DT, I)          \
+  do {                              \
+    if (past) GA_ROT(DT, I, true);  \
+    else GA_ROT(DT, I, false);      \
+  } while (0)
   if (dtype == 1) {
-    if (interleaved) GA_ROT(BF16, true);
-    else GA_ROT(BF16, false);
+    if (interleaved) GA_ROT_PAST(BF16, true);
+    else GA_ROT_PAST(BF16, false);
   } else {
-    if (interleaved) GA_ROT(F32, true);
-    else GA_ROT(F32, false);
+    if (interleaved) GA_ROT_PAST(F32, true);
+    else GA_ROT_PAST(F32, false);
   }
+#undef GA_ROT_PAST
 #undef GA_ROT
   return hipGetLastError();
 }
