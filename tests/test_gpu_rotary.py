@@ -116,3 +116,19 @@ def test_copied_pairs_bit_for_bit(dev, dtype, interleaved):
     assert torch.equal(got[..., last].contiguous().view(bits), Q[..., last].contiguous().view(bits))
     rest = [i for i in range(64) if i not in last]
     assert torch.isfinite(got[..., rest]).all()
+
+
+@pytest.mark.parametrize("dtype,n", [("bf16", 200000), ("f32", 100000)])
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_outputs_larger_than_the_caches(dev, dtype, n, interleaved):
+    """Written past the caches (205 MB of outputs), in place as well: the bits of a small call."""
+    g = torch.Generator(device=dev).manual_seed(4)
+    Q = torch.randn(1, 8, n, 64, device=dev, generator=g).to(DT[dtype])
+    pos = torch.arange(n, dtype=torch.int32, device=dev).view(1, 1, n)
+    whole = ga.rotary(Q, None, pos, (32,), interleaved=interleaved)
+    for h, at in ((0, 0), (3, n // 2), (7, n - 50)):
+        part = ga.rotary(Q[:, h:h + 1, at:at + 50].contiguous(), None, pos[:, :, at:at + 50].contiguous(), (32,),
+                         interleaved=interleaved)
+        assert torch.equal(whole[:, h:h + 1, at:at + 50], part)
+    ga.rotary(Q, None, pos, (32,), interleaved=interleaved, out=(Q, None))
+    assert torch.equal(Q, whole)
